@@ -323,6 +323,104 @@ rp_status inram_train_steps(inram_replay_t* h, trainer_t* tr, uint64_t count,
 rp_status inram_get_state(inram_replay_t* h, uint64_t* head, uint64_t* size, uint64_t* total,
                           uint64_t* step);
 
+/*
+ * Operators on rows of logits: what a program does with a network's output rows besides training on
+ * them by temporal differences.  A row holds one logit per action; a Q-value serves as one
+ * (softmax over Q / temperature is Boltzmann exploration).  They take any rows the caller has, of
+ * 1 to 262,144 actions, keep no state, allocate nothing and may be captured into a graph.
+ * Two calls that may overlap in time (two streams, two captured graphs) need a workspace each.
+ */
+typedef struct {
+    const void* data;     /* device: element (i, j) is data[i * stride + j], aligned to its type */
+    uint64_t rows;        /* up to 2^24; 0 = nothing is done                                     */
+    uint64_t stride;      /* elements from a row to the next (0: every row is the same one)      */
+    uint32_t n;           /* actions per row, 1 .. 262,144                                       */
+    uint32_t dtype;       /* RP_F32 | RP_BF16                                                    */
+} rp_rows;
+
+/* How actions are chosen; each setting is one value for all rows or, where its array (device,
+ * [rows]) is not NULL, one per row. */
+typedef struct {
+    double temperature;             /* logits are divided by it; not > 0 (or NaN): the best action  */
+    double top_p;                   /* see rp_choose_actions; not < 1: off                          */
+    double min_p;                   /* not > 0: off                                                 */
+    int64_t top_k;                  /* not in 1 .. n - 1: off                                       */
+    const float* row_temperature;
+    const float* row_top_p;
+    const float* row_min_p;
+    const int32_t* row_top_k;
+} rp_choice;
+
+/* Bytes of device workspace rp_choose_actions needs (0 is a valid answer; (size_t)-1 if the rows are
+ * invalid).  Pure host arithmetic. */
+size_t rp_choose_workspace_bytes(const rp_rows* logits);
+
+/*
+ * Choose one action per row from given random numbers u[rows] in [0, 1).  An action is allowed
+ * unless its logit is -infinity or NaN.  With the allowed ones in order of falling logit (equal ones:
+ * lower index first), w_j = exp((x_j - x_0) / temperature) and C_j = w_0 + .. + w_j, an action stays
+ * in if it is among the first top_k, the sum before it is less than top_p times the sum over those
+ * top_k, and w_j >= min_p; the first always stays.  The choice is the first j with C_j > u * M, M
+ * the sum over those that stay, or the last of them if there is none.
+ * index[rows]: the action, or -1 where no action is allowed.  logp[rows] (may be NULL): the logarithm
+ * of its probability w_j / M (0 for index -1 and for the best action at temperature 0).
+ * Weights and sums are held in 64 bits, and sums do not depend on the order in which the GPU's
+ * workgroups run: the same call gives the same bits.  Logits of +infinity share all weight equally.
+ */
+rp_status rp_choose_actions(const rp_rows* logits, const rp_choice* how, const float* u, int32_t* index,
+                            float* logp, void* workspace, size_t bytes, void* hip_stream);
+
+/* Bytes of device workspace rp_top_actions needs for k actions per row ((size_t)-1 if invalid). */
+size_t rp_top_workspace_bytes(const rp_rows* logits, uint32_t k);
+
+/*
+ * The k (1 .. min(n, 1024)) largest logits of every row, in the order of rp_choose_actions:
+ * values[rows * k] in the logits' type and index[rows * k]; past the last allowed action -infinity and
+ * -1.  lse[rows] (may be NULL): log sum_j exp(x_j / temperature) over the whole row, with
+ * a finite temperature > 0 (-infinity for a row without an allowed action).  What a teacher
+ * writes down for rp_distill_loss.
+ */
+rp_status rp_top_actions(const rp_rows* logits, uint32_t k, double temperature, void* values, int32_t* index,
+                         float* lse, void* workspace, size_t bytes, void* hip_stream);
+
+/* A teacher's top logits, k (1 .. 1024) entries per row; all arrays are device memory. */
+typedef struct {
+    const void* value;          /* [rows * k] logits                                                  */
+    const int32_t* index;       /* [rows * k] their actions; one outside 0 .. n - 1 is no entry       */
+    const float* lse;           /* [rows] log-sum-exp of the teacher's whole row at its temperature, or NULL */
+    const float* weight;        /* [rows] what a row's loss and gradient are multiplied by, or NULL (1).
+                                   A row of weight 0 is not read: loss 0, gradient 0                  */
+    uint32_t k;
+    uint32_t dtype;             /* of value: RP_F32 | RP_BF16                                         */
+    double temperature;         /* the teacher's, finite > 0                                          */
+    double student_temperature; /* finite > 0                                                         */
+} rp_teacher;
+
+/* Bytes of device workspace rp_distill_loss and rp_distill_grad need ((size_t)-1 if invalid). */
+size_t rp_distill_workspace_bytes(const rp_rows* logits, uint32_t k);
+
+/*
+ * Distillation from a teacher's top logits.  With p = softmax(student's row / student_temperature) and
+ * entry e of action j_e carrying q_e:
+ *   lse NULL:  q = softmax(value / temperature) over the row's entries;
+ *   else:      q_e = exp(value_e / temperature - lse), and what is missing from 1 is the teacher's mass
+ *              outside its entries, set against the student's p_rest there as one more event;
+ *   loss = sum_e q_e (log q_e - log p[j_e])  [ + q_rest (log q_rest - log p_rest) ],
+ * times the row's weight.  The last term is left out where q_rest <= 0 or p_rest = 0.  Entries with q_e = 0
+ * add nothing; two entries of one action both count.  A row without entries or without an allowed
+ * action in the student's row has loss 0 and gradient 0.  NaN and +infinity among the logits of a row
+ * of weight other than 0, or among its entries' values, make its loss and its gradient NaN.
+ */
+rp_status rp_distill_loss(const rp_rows* logits, const rp_teacher* teacher, float* loss, void* workspace,
+                          size_t bytes, void* hip_stream);
+
+/* The same loss, and its gradient with respect to the student's logits:
+ *   grad_i = weight / student_temperature * (p_i Q - sum of q_e with j_e = i  - [i in no entry] q_rest p_i / p_rest),
+ * Q = sum_e q_e [+ q_rest].  grad (device): element (i, j) at grad[i * grad_stride + j], of the logits' type;
+ * it may be the logits' own memory at the same stride, and may not overlap it otherwise. */
+rp_status rp_distill_grad(const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad,
+                          uint64_t grad_stride, void* workspace, size_t bytes, void* hip_stream);
+
 /* Message for the last failure on this thread ("" if none). */
 const char* rp_last_error(void);
 /* Library version string. */

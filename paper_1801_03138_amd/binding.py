@@ -49,6 +49,23 @@ class TrainConfig(C.Structure):
                 ("head", C.c_uint32), ("hidden2", C.c_uint32)]
 
 
+class LogitRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("stride", C.c_uint64), ("n", C.c_uint32),
+                ("dtype", C.c_uint32)]
+
+
+class Choice(C.Structure):
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double),
+                ("top_k", C.c_int64), ("row_temperature", C.c_void_p), ("row_top_p", C.c_void_p),
+                ("row_min_p", C.c_void_p), ("row_top_k", C.c_void_p)]
+
+
+class Teacher(C.Structure):
+    _fields_ = [("value", C.c_void_p), ("index", C.c_void_p), ("lse", C.c_void_p), ("weight", C.c_void_p),
+                ("k", C.c_uint32), ("dtype", C.c_uint32), ("temperature", C.c_double),
+                ("student_temperature", C.c_double)]
+
+
 # every symbol include/ingpu_replay.h declares: name -> (restype, argtypes)
 _vp, _u32, _u64, _int = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int
 SYMBOLS = {
@@ -85,6 +102,13 @@ SYMBOLS = {
     "train_kernels_per_step": (_int, [_vp, _vp]),
     "train_set_handoff_wait": (_int, [_vp, _u64, _int]),
     "train_get_target_source": (_int, [_vp, _vp]),
+    "rp_choose_workspace_bytes": (C.c_size_t, [_vp]),
+    "rp_choose_actions": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "rp_top_workspace_bytes": (C.c_size_t, [_vp, _u32]),
+    "rp_top_actions": (_int, [_vp, _u32, C.c_double, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "rp_distill_workspace_bytes": (C.c_size_t, [_vp, _u32]),
+    "rp_distill_loss": (_int, [_vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "rp_distill_grad": (_int, [_vp, _vp, _vp, _vp, _u64, _vp, C.c_size_t, _vp]),
     "rp_last_error": (C.c_char_p, []),
     "rp_version": (C.c_char_p, []),
 }
@@ -489,3 +513,163 @@ class InRamReplay:
         v = [C.c_uint64() for _ in range(4)]
         _check(lib().inram_get_state(self._h, *[C.byref(x) for x in v]))
         return tuple(x.value for x in v)
+
+
+# ------------------------------------------------------------------- operators on rows of logits
+_LOGIT_DTYPE = {torch.float32: RP_F32, torch.bfloat16: RP_BF16}
+_INVALID = C.c_size_t(-1).value
+
+
+def check_rows(t, what, device_type="cuda"):
+    """rows x n logits: a 2-D tensor of float32 or bfloat16 whose rows are contiguous, at any row stride."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _LOGIT_DTYPE:
+        raise ValueError(f"{what}: expected a rows x n tensor of float32 or bfloat16")
+    if t.device.type != device_type:
+        raise ValueError(f"{what}: tensor is on {t.device}, not on the GPU")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: a row's elements are not contiguous")
+    return t
+
+
+def check_setting(v, dtype, rows, device, what):
+    """One value for all rows, or a device array with one per row: (value, tensor or None)."""
+    if isinstance(v, torch.Tensor):
+        return None, check_device_array(v, (dtype,), rows, device, what)
+    return v, None
+
+
+def _logit_rows(t):
+    return LogitRows(t.data_ptr(), t.shape[0], t.stride(0), t.shape[1], _LOGIT_DTYPE[t.dtype])
+
+
+class _On:
+    """The device of a call's tensors as the current one and, if a stream is given, that stream for what the
+    call allocates; nothing to do for most calls."""
+
+    def __init__(self, device, stream):
+        self._hold = []
+        if device.index is not None and device.index != torch.cuda.current_device():
+            self._hold.append(torch.cuda.device(device))
+        if stream is not None:
+            self._hold.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for h in self._hold:
+            h.__enter__()
+
+    def __exit__(self, *error):
+        for h in reversed(self._hold):
+            h.__exit__(*error)
+
+
+def _workspace(nbytes, workspace, device, what):
+    """The call's workspace: the caller's, or one allocated on the current stream; (tensor, address, bytes)."""
+    if nbytes == _INVALID:
+        raise ReplayError(RP_EINVAL, lib().rp_last_error().decode())
+    if workspace is not None:
+        check_device_array(workspace, (torch.uint8,), workspace.numel(), device, what + ": workspace")
+    elif nbytes:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return (workspace, None, 0) if workspace is None else (workspace, workspace.data_ptr(), workspace.numel())
+
+
+def choose_actions(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, workspace=None, stream=None):
+    """One action per row of logits (or Q-values) from the random numbers u[rows] in [0, 1): see
+    rp_choose_actions.  Each setting is a number, or a device tensor with one per row (float32; top_k int32).
+    Returns (index int32[rows], logp float32[rows]), in `out` if given."""
+    check_rows(logits, "choose_actions: logits")
+    rows, dev = logits.shape[0], logits.device
+    check_device_array(u, (torch.float32,), rows, dev, "choose_actions: u")
+    t, t_row = check_setting(temperature, torch.float32, rows, dev, "choose_actions: temperature")
+    k, k_row = check_setting(top_k, torch.int32, rows, dev, "choose_actions: top_k")
+    p, p_row = check_setting(top_p, torch.float32, rows, dev, "choose_actions: top_p")
+    m, m_row = check_setting(min_p, torch.float32, rows, dev, "choose_actions: min_p")
+    with _On(dev, stream):
+        if out is None:
+            out = (torch.empty(rows, dtype=torch.int32, device=dev), torch.empty(rows, dtype=torch.float32, device=dev))
+        index, logp = out
+        check_device_array(index, (torch.int32,), rows, dev, "choose_actions: index")
+        if logp is not None:
+            check_device_array(logp, (torch.float32,), rows, dev, "choose_actions: logp")
+        x = _logit_rows(logits)
+        how = Choice(1.0 if t is None else t, 1.0 if p is None else p, 0.0 if m is None else m, 0 if k is None else k,
+                     _dev(t_row), _dev(p_row), _dev(m_row), _dev(k_row))
+        hold, ws, nbytes = _workspace(lib().rp_choose_workspace_bytes(C.byref(x)), workspace, dev, "choose_actions")
+        _check(lib().rp_choose_actions(C.byref(x), C.byref(how), u.data_ptr(), index.data_ptr(), _dev(logp), ws, nbytes,
+                                       _stream_ptr(stream)))
+    return index, logp
+
+
+def top_actions(logits, k, temperature=1.0, out=None, workspace=None, stream=None):
+    """The k largest logits of every row, their actions, and the row's log-sum-exp at a temperature: see
+    rp_top_actions.  Returns (values [rows, k] in the logits' type, index int32[rows, k], lse float32[rows])."""
+    check_rows(logits, "top_actions: logits")
+    rows, dev = logits.shape[0], logits.device
+    with _On(dev, stream):
+        x = _logit_rows(logits)
+        need = lib().rp_top_workspace_bytes(C.byref(x), k)
+        hold, ws, nbytes = _workspace(need, workspace, dev, "top_actions")
+        if out is None:
+            out = (torch.empty((rows, k), dtype=logits.dtype, device=dev),
+                   torch.empty((rows, k), dtype=torch.int32, device=dev),
+                   torch.empty(rows, dtype=torch.float32, device=dev))
+        values, index, lse = out
+        check_device_array(values, (logits.dtype,), rows * k, dev, "top_actions: values")
+        check_device_array(index, (torch.int32,), rows * k, dev, "top_actions: index")
+        if lse is not None:
+            check_device_array(lse, (torch.float32,), rows, dev, "top_actions: lse")
+        _check(lib().rp_top_actions(C.byref(x), k, temperature, values.data_ptr(), index.data_ptr(), _dev(lse), ws,
+                                    nbytes, _stream_ptr(stream)))
+    return values, index, lse
+
+
+def _teacher(logits, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, what):
+    check_rows(logits, what + ": logits")
+    rows, dev = logits.shape[0], logits.device
+    if not isinstance(index, torch.Tensor) or index.dim() != 2 or index.shape[0] != rows:
+        raise ValueError(f"{what}: index must be a rows x k tensor")
+    k = index.shape[1]
+    check_device_array(index, (torch.int32,), rows * k, dev, what + ": index")
+    check_device_array(teacher, tuple(_LOGIT_DTYPE), rows * k, dev, what + ": teacher")
+    if teacher_lse is not None:
+        check_device_array(teacher_lse, (torch.float32,), rows, dev, what + ": teacher_lse")
+    if weight is not None:
+        check_device_array(weight, (torch.float32,), rows, dev, what + ": weight")
+    return _logit_rows(logits), Teacher(teacher.data_ptr(), index.data_ptr(), _dev(teacher_lse), _dev(weight), k,
+                                        _LOGIT_DTYPE[teacher.dtype], teacher_temperature, student_temperature)
+
+
+def distill_loss(logits, teacher, index, weight=None, teacher_lse=None, student_temperature=1.0,
+                 teacher_temperature=1.0, out=None, workspace=None, stream=None):
+    """Loss of every row of the student's logits against a teacher's top logits [rows, k] and their actions, as
+    top_actions returns them: see rp_distill_loss.  Returns float32[rows]."""
+    rows, dev = len(logits), logits.device
+    x, t = _teacher(logits, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_loss")
+    with _On(dev, stream):
+        hold, ws, nbytes = _workspace(lib().rp_distill_workspace_bytes(C.byref(x), t.k), workspace, dev, "distill_loss")
+        out = torch.empty(rows, dtype=torch.float32, device=dev) if out is None else out
+        check_device_array(out, (torch.float32,), rows, dev, "distill_loss: out")
+        _check(lib().rp_distill_loss(C.byref(x), C.byref(t), out.data_ptr(), ws, nbytes, _stream_ptr(stream)))
+    return out
+
+
+def distill_grad(logits, teacher, index, weight=None, teacher_lse=None, student_temperature=1.0,
+                 teacher_temperature=1.0, out=None, workspace=None, stream=None):
+    """distill_loss and its gradient with respect to the logits: see rp_distill_grad.  Returns (loss float32[rows],
+    gradient [rows, n] in the logits' type); `out` = (loss, gradient), the gradient at any row stride, also
+    the logits themselves."""
+    rows, dev = len(logits), logits.device
+    x, t = _teacher(logits, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_grad")
+    with _On(dev, stream):
+        hold, ws, nbytes = _workspace(lib().rp_distill_workspace_bytes(C.byref(x), t.k), workspace, dev, "distill_grad")
+        if out is None:
+            out = (torch.empty(rows, dtype=torch.float32, device=dev),
+                   torch.empty((rows, logits.shape[1]), dtype=logits.dtype, device=dev))
+        loss, grad = out
+        check_device_array(loss, (torch.float32,), rows, dev, "distill_grad: loss")
+        check_rows(grad, "distill_grad: gradient")
+        if grad.shape != logits.shape or grad.dtype != logits.dtype or grad.device != dev:
+            raise ValueError("distill_grad: the gradient's shape, type and device must be the logits'")
+        _check(lib().rp_distill_grad(C.byref(x), C.byref(t), loss.data_ptr(), grad.data_ptr(), grad.stride(0), ws, nbytes,
+                                     _stream_ptr(stream)))
+    return loss, grad

@@ -1,0 +1,102 @@
+// Rows of logits: what the operators on them share on the device and on the host.
+#pragma once
+
+#include <cmath>
+
+#include "common.hpp"
+
+namespace rp {
+
+constexpr unsigned int kMaxActions = 1u << 18;   // a row's length
+constexpr unsigned int kMaxTop = 1024;           // entries of a teacher's row
+constexpr unsigned long long kMaxLogitRows = 1ull << 24;
+
+struct LogitRows {
+    const unsigned char* data;
+    unsigned long long rows, stride;
+    unsigned int n;
+};
+
+__device__ __forceinline__ float logit_value(const float* p) { return *p; }
+__device__ __forceinline__ float logit_value(const unsigned short* p) { return __uint_as_float((unsigned int)*p << 16); }
+
+// What is not allowed (NaN, -infinity) becomes -infinity and -0 becomes +0, so that equal logits have
+// equal keys.
+__device__ __forceinline__ float clean_logit(float x) { return fmaxf(x, -INFINITY) + 0.f; }
+
+// Unsigned integers in the order of the floats.
+__device__ __forceinline__ unsigned int order_key(float x) {
+    const unsigned int b = __float_as_uint(x);
+    return b ^ ((unsigned int)((int)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(unsigned int k) {
+    return __uint_as_float(k ^ ((unsigned int)((int)~k >> 31) | 0x80000000u));
+}
+constexpr unsigned int kMaskedKey = 0x007FFFFFu;   // order_key(-infinity)
+
+// An action in the order of choice as one number, the first the largest: falling logit, rising index.
+__device__ __forceinline__ unsigned long long order_word(unsigned int key, unsigned int index) {
+    return (unsigned long long)key << 32 | (0xFFFFFFFFu - index);
+}
+__device__ __forceinline__ unsigned int word_index(unsigned long long w) { return 0xFFFFFFFFu - (unsigned int)w; }
+__device__ __forceinline__ unsigned int word_key(unsigned long long w) { return (unsigned int)(w >> 32); }
+
+// -log of an allowed action's weight: (m - x) / temperature.  The row's maximum m may be +infinity; a logit equal
+// to it has weight 1 whatever the temperature, any other is then infinitely far away.
+__device__ __forceinline__ double logit_depth(float m, float x, double inv_t) {
+    return x == m ? 0.0 : isinf(m) ? (double)INFINITY : ((double)m - (double)x) * inv_t;
+}
+
+struct MaxOp {
+    template <typename V>
+    __device__ V operator()(V a, V b) const { return a > b ? a : b; }
+};
+struct MinOp {
+    template <typename V>
+    __device__ V operator()(V a, V b) const { return a < b ? a : b; }
+};
+struct SumOp {
+    template <typename V>
+    __device__ V operator()(V a, V b) const { return a + b; }
+};
+
+template <typename V, typename Op>
+__device__ __forceinline__ V wave_reduce(V v, Op op) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v = op(v, __shfl_xor(v, off, 64));
+    return v;
+}
+
+// The same value in every thread of a workgroup of W wavefronts, combined in a fixed order.  `part` holds W
+// values; a barrier has to stand between two uses of it.
+template <int W, typename V, typename Op>
+__device__ __forceinline__ V block_reduce(V v, Op op, V* part) {
+    v = wave_reduce(v, op);
+    if (W == 1) return v;
+    if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    V all = part[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) all = op(all, part[w]);
+    return all;
+}
+
+// Host side: rows that the kernels can be given, or why not.
+inline const char* logit_rows_fault(const rp_rows* r) {
+    if (!r) return "null rows";
+    if (r->dtype != RP_F32 && r->dtype != RP_BF16) return "logits must be RP_F32 or RP_BF16";
+    if (r->n == 0 || r->n > kMaxActions) return "a row holds 1 to 262144 actions";
+    if (r->rows > kMaxLogitRows) return "more than 2^24 rows";
+    if (r->stride > (1ull << 40)) return "row stride beyond 2^40";
+    return nullptr;
+}
+inline const char* logit_data_fault(const rp_rows* r) {
+    if (!r->data) return "null logits";
+    if (reinterpret_cast<uintptr_t>(r->data) & (r->dtype == RP_BF16 ? 1u : 3u)) return "logits not aligned to their type";
+    return nullptr;
+}
+inline LogitRows logit_rows(const rp_rows* r) {
+    return LogitRows{static_cast<const unsigned char*>(r->data), r->rows, r->stride, r->n};
+}
+
+}  // namespace rp

@@ -1,0 +1,447 @@
+"""Operators on rows of logits on the GPU against their definitions in 64 bits (tests/logits_ref.py)."""
+import math
+import os
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import logits_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+INF = math.inf
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_1801_03138_amd import binding
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    binding.lib()
+    return binding
+
+
+def table(rng, rows, n, dtype, pad=0, sigma=1.5, masked=0.0, shift=0.0):
+    """rows x n logits on the GPU as a view into a wider table, and the same values in 64 bits."""
+    x = rng.normal(shift, sigma, (rows, n + pad)).astype(np.float32)
+    if masked:
+        x[rng.random(x.shape) < masked] = -INF
+    t = torch.from_numpy(x).to(DT[dtype]).cuda()
+    view = t[:, :n]
+    return view, view.float().cpu().double().numpy()
+
+
+# --------------------------------------------------------------------------------------- choose
+def check_choice(x, u, how, index, logp):
+    """Every row's choice is the definition's; where u falls within a hair of a border, either neighbour.
+    Sums are off by less than half a unit of 2^-44 (of the best action's weight) per action, and by a few
+    2^-53 of themselves; the log-probability is rounded to 32 bits once."""
+    index, logp = index.cpu().numpy(), logp.cpu().double().numpy()
+    for r in range(len(x)):
+        row_how = {k: float(v[r]) if isinstance(v, np.ndarray) else v for k, v in how.items()}
+        row_how["top_k"] = int(row_how.get("top_k", 0))
+        want = ref.choose(x[r], float(u[r]), **row_how)
+        if want is None:
+            assert index[r] == -1 and logp[r] == 0, r
+            continue
+        ids, c, at = want
+        hair = len(x[r]) * 2.0 ** -44 + 2.0 ** -40 * c[-1]
+        drawn = max(float(u[r]), 0.0) * c[-1]
+        near = [at]
+        if at > 0 and drawn - c[at - 1] < hair:
+            near.append(at - 1)
+        if at + 1 < len(c) and c[at] - drawn < hair:
+            near.append(at + 1)
+        assert index[r] in ids[near], (r, index[r], ids[near], row_how, float(u[r]))
+        got = int(np.nonzero(ids == index[r])[0][0])
+        w = c[got] - (c[got - 1] if got else 0.0)
+        exact = math.log(w / c[-1]) if row_how.get("temperature", 1.0) > 0 else 0.0
+        assert abs(logp[r] - exact) <= 2.0 ** -23 * abs(exact) + 2 * hair / w, (r, logp[r], exact)
+
+
+def draw_u(rng, rows):
+    u = rng.random(rows).astype(np.float32)
+    edge = np.array([0.0, np.float32(1 - 2.0 ** -24), 0.5], np.float32)
+    u[:min(rows, 3)] = edge[:min(rows, 3)]
+    return u
+
+
+SHAPES = [(1, 1), (3, 2), (130, 30), (5, 63), (5, 64), (5, 65), (7, 257), (4, 1000), (3, 2049), (9, 4099), (2, 20_011),
+          (1, 131_072), (3, 70_001)]
+HOWS = [{"temperature": 0.8}, {"temperature": 1.3, "top_k": 7}, {"top_p": 0.9}, {"top_p": 0.7, "min_p": 0.01, "top_k": 50},
+        {"min_p": 0.2}, {"temperature": 0.0}, {"top_k": 1}, {"top_p": 0.0}, {"temperature": 0.7, "top_k": 1500, "top_p": 0.97},
+        {"temperature": 4.0, "top_k": 1024}]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", SHAPES)
+def test_choice_is_the_definitions(B, rows, n, dtype):
+    rng = np.random.default_rng(rows * 1000 + n)
+    for i, how in enumerate(HOWS):
+        g, x = table(rng, rows, n, dtype, pad=[0, 1, 2, 5][i % 4], sigma=[0.3, 1.5, 3.0][i % 3], masked=[0.0, 0.4][i % 2],
+                     shift=[0.0, -7.0, 40.0][(i // 2) % 3])
+        u = draw_u(rng, rows)
+        index, logp = B.choose_actions(g, torch.from_numpy(u).cuda(), **how)
+        check_choice(x, u, how, index, logp)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(200, 30), (40, 700), (24, 5003), (9, 33_333)])
+def test_every_row_has_its_own_settings(B, rows, n, dtype):
+    rng = np.random.default_rng(n)
+    g, x = table(rng, rows, n, dtype, pad=3, sigma=2.0, masked=0.2)
+    how = {"temperature": rng.choice([-1.0, 0.0, 0.5, 1.0, 2.5, 1e-30, 1e30], rows).astype(np.float32),
+           "top_k": rng.choice([-3, 0, 1, 2, 20, 300, 1024, 1025, n, n + 1], rows).astype(np.int32),
+           "top_p": rng.choice([-1.0, 0.0, 0.1, 0.5, 0.95, 1.0, 2.0], rows).astype(np.float32),
+           "min_p": rng.choice([-1.0, 0.0, 0.001, 0.3, 1.0, 1.5], rows).astype(np.float32)}
+    u = draw_u(rng, rows)
+    index, logp = B.choose_actions(g, torch.from_numpy(u).cuda(), **{k: torch.from_numpy(v).cuda() for k, v in how.items()})
+    check_choice(x, u, how, index, logp)
+
+
+SPECIAL = {
+    "nothing allowed": lambda n: [-INF] * n,
+    "only NaN": lambda n: [math.nan] * n,
+    "one allowed": lambda n: [-INF] * (n - 1) + [-3.0],
+    "NaN among others": lambda n: [math.nan, 1.0] + [0.5] * (n - 2),
+    "infinities": lambda n: [0.0, INF, 5.0, INF] + [-INF] * (n - 4),
+    "all equal": lambda n: [0.25] * n,
+    "both zeros": lambda n: [0.0, -0.0] * (n // 2) + [0.0] * (n % 2),
+    "lowest values": lambda n: [-3.3895313892515355e38] * (n - 2) + [0.0, -1.0],
+    "only lowest values": lambda n: [-3.3895313892515355e38] * n,
+    "highest and lowest": lambda n: [3.3895313892515355e38] * 2 + [-3.3895313892515355e38] * (n - 2),
+    "two levels": lambda n: [1.0] * (n // 2) + [2.0] * (n - n // 2),
+    "a far tail": lambda n: [30.0] + [0.0] * (n - 1),
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [6, 30, 64, 65, 1000, 6001, 150_001])
+def test_choice_from_special_rows(B, n, dtype):
+    names = list(SPECIAL)
+    g = torch.tensor([SPECIAL[k](n) for k in names], dtype=torch.float32).to(DT[dtype]).cuda()
+    x = g.float().cpu().double().numpy()
+    for u0 in (0.0, 0.25, 0.5, 1 - 2.0 ** -24):
+        u = np.full(len(names), u0, np.float32)
+        for how in ({}, {"top_k": 3}, {"top_k": 1000}, {"top_k": 1500}, {"top_p": 0.5}, {"min_p": 0.5}, {"temperature": 0.0},
+                    {"temperature": INF}, {"temperature": math.nan}, {"top_p": math.nan, "min_p": math.nan}):
+            index, logp = B.choose_actions(g, torch.from_numpy(u).cuda(), **how)
+            check_choice(np.where(np.isnan(x), -INF, x), u, how, index, logp)
+
+
+def test_random_numbers_outside_the_unit_interval_are_its_ends(B):
+    g, x = table(np.random.default_rng(1), 1, 40, "f32")
+    c = lambda v: int(B.choose_actions(g, torch.tensor([v], device="cuda"))[0])
+    first, last = c(0.0), ref.order(x[0])[-1]
+    assert first == ref.order(x[0])[0]
+    assert c(-1.0) == first and c(math.nan) == first and c(1.0) == last and c(7.0) == last
+
+
+@pytest.mark.parametrize("n", [30, 6007])
+def test_choices_have_the_softmax_frequencies(B, n):
+    """Evenly spaced random numbers hit every action as often as its probability says, to one draw."""
+    rng = np.random.default_rng(5)
+    g, x = table(rng, 1, n, "f32", sigma=2.0)
+    draws = 20_000
+    u = ((np.arange(draws) + 0.5) / draws).astype(np.float32)
+    index = B.choose_actions(g.expand(draws, n), torch.from_numpy(u).cuda())[0].cpu().numpy()
+    p = np.exp(x[0] - ref.log_sum_exp(x[0]))
+    # (u is rounded to 2^-24: a draw moves by less than 2^-24 * draws of a place)
+    assert np.abs(np.bincount(index, minlength=n) - p * draws).max() <= 1.01
+
+
+# ------------------------------------------------------------------------------------------ top
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", SHAPES)
+def test_top_actions(B, rows, n, dtype):
+    rng = np.random.default_rng(rows * 77 + n)
+    for i, k in enumerate(sorted({1, 2, 8, 64, 100, 500, 1000, 1024, n})):
+        if k > min(n, 1024):
+            continue
+        g, x = table(rng, rows, n, dtype, pad=i % 3, sigma=[0.3, 2.0][i % 2], masked=[0.0, 0.5, 0.0, 0.97][i % 4])
+        t = [1.0, 0.7, 3.0][i % 3]
+        check_top(x, k, t, *B.top_actions(g, k, temperature=t))
+
+
+def check_top(x, k, t, values, index, lse):
+    values, index, lse = values.float().cpu().numpy(), index.cpu().numpy(), lse.cpu().numpy()
+    for r in range(len(x)):
+        ids = ref.order(x[r])[:k]
+        assert np.array_equal(index[r], np.concatenate([ids, np.full(k - len(ids), -1)])), r
+        assert np.array_equal(values[r], np.concatenate([x[r][ids], np.full(k - len(ids), -INF)])), r
+        if len(ids) and x[r][ids[0]] == INF:
+            assert lse[r] == INF
+            continue
+        want = ref.log_sum_exp(x[r], t)
+        if want == -INF:
+            assert lse[r] == -INF
+            continue
+        # the sum's relative error (see ref.distill), and the rounding of the result
+        assert abs(lse[r] - want) <= 2.0 ** -22 * (math.log(x.shape[1]) + 4) + 2.0 ** -23 * abs(want), (r, lse[r], want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [6, 30, 64, 65, 1000, 6001, 150_001])
+def test_top_actions_of_special_rows(B, n, dtype):
+    names = list(SPECIAL)
+    g = torch.tensor([SPECIAL[k](n) for k in names], dtype=torch.float32).to(DT[dtype]).cuda()
+    x = g.float().cpu().double().numpy()
+    for k in {1, 5, min(n, 700), min(n, 1024)}:
+        check_top(np.where(np.isnan(x), -INF, x), k, 1.0, *B.top_actions(g, k))
+
+
+# -------------------------------------------------------------------------------------- distill
+def entries(rng, x, k, dtype, short=0.2, repeated=False, noise=1.0):
+    """A teacher's entries for rows x: the top k of noisy logits, some missing; its log-sum-exp at 0.9."""
+    rows, n = x.shape
+    t = 0.7 * np.where(np.isfinite(x), x, 0.0) + rng.normal(0, noise, x.shape)
+    t = torch.from_numpy(t.astype(np.float32)).to(DT[dtype]).double().numpy()
+    index = np.argsort(-t, axis=1, kind="stable")[:, :k].astype(np.int32)
+    if k > n:
+        index = np.concatenate([index, np.full((rows, k - n), -1, np.int32)], axis=1)
+    value = np.take_along_axis(t, np.maximum(index, 0), 1)
+    lse = np.array([ref.log_sum_exp(r, 0.9) for r in t], np.float32)
+    index[rng.random(index.shape) < short] = rng.choice([-1, n, n + 5, -(2 ** 31), 2 ** 31 - 1])
+    if repeated and k > 1:
+        index[:, -1] = index[:, 0]
+        index[::2, k // 2] = index[::2, 0]
+        lse += 0.5   # (so that the entries' mass stays below 1)
+    return value, index, lse
+
+
+def check_distill(B, g, x, value, index, weight, lse, tdtype, dtype, ts=1.1, tt=0.9):
+    tv = torch.from_numpy(value.astype(np.float32)).to(DT[tdtype])
+    value = tv.double().numpy()
+    kw = dict(weight=None if weight is None else torch.from_numpy(weight).cuda(),
+              teacher_lse=None if lse is None else torch.from_numpy(lse).cuda(), student_temperature=ts,
+              teacher_temperature=tt)
+    idx = torch.from_numpy(index).cuda()
+    only = B.distill_loss(g, tv.cuda(), idx, **kw)
+    loss, grad = B.distill_grad(g, tv.cuda(), idx, **kw)
+    own = g.clone()
+    own_loss, own_grad = B.distill_grad(own, tv.cuda(), idx, out=(torch.empty_like(loss), own), **kw)
+    assert own_grad.data_ptr() == own.data_ptr()
+    assert torch.equal(own_loss, loss) and torch.equal(own_grad.float().nan_to_num(7.0), grad.float().nan_to_num(7.0))
+    grad, loss, only = grad.double().cpu().numpy(), loss.double().cpu().numpy(), only.double().cpu().numpy()
+    half = torch.finfo(DT[dtype]).eps / 2
+    tiny = float(torch.finfo(DT[dtype]).tiny)
+    for r in range(len(x)):
+        want, dwant, slack, dslack = ref.distill(x[r], value[r], index[r], 1.0 if weight is None else float(weight[r]),
+                                                 None if lse is None else float(lse[r]), ts, tt)
+        for got in (loss[r], only[r]):
+            assert got == want or abs(got - want) <= slack + 1e-12, (r, got, want, slack)
+        off = np.abs(grad[r] - dwant) - (dslack + (half + 2.0 ** -23) * np.abs(dwant) + tiny)
+        assert (off <= 0).all(), (r, int(off.argmax()), grad[r][off.argmax()], dwant[off.argmax()], float(off.max()))
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype,tdtype", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("rows,n,k", [(1, 1, 1), (3, 2, 1), (130, 30, 8), (5, 64, 64), (5, 65, 3), (7, 257, 300), (4, 1000, 1000),
+                                      (3, 2049, 17), (9, 4099, 64), (2, 20_011, 1024), (1, 131_072, 50), (3, 70_001, 333),
+                                      (600, 1031, 5)])
+def test_distillation(B, rows, n, k, dtype, tdtype, rest):
+    rng = np.random.default_rng(rows + n + k)
+    for i in range(2):
+        g, x = table(rng, rows, n, dtype, pad=[0, 3][i], sigma=[2.0, 0.2][i], shift=[0.0, 20.0][i])
+        value, index, lse = entries(rng, x, k, tdtype, short=[0.0, 0.3][i])
+        weight = rng.choice([0.0, 1.0, -0.5, 1.0 / rows], rows).astype(np.float32) if i else None
+        check_distill(B, g, x, value, index, weight, lse if rest else None, tdtype, dtype)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("n,k", [(30, 7), (5000, 40), (90_001, 1000)])
+def test_distillation_with_an_action_in_several_entries(B, n, k, rest):
+    rng = np.random.default_rng(n)
+    g, x = table(rng, 5, n, "f32")
+    value, index, lse = entries(rng, x, k, "f32", short=0.1, repeated=True)
+    check_distill(B, g, x, value, index, None, lse if rest else None, "f32", "f32")
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("n", [30, 1500, 80_000])
+def test_distillation_of_masked_rows(B, n, rest):
+    """Student's actions that are not allowed, teachers without entries, rows without either."""
+    rng = np.random.default_rng(n)
+    g, x = table(rng, 6, n, "f32")
+    value, index, lse = entries(rng, x, 5, "f32", short=0.0)
+    outside = [a for a in range(n) if a not in index[0]][:3]
+    g[0, outside] = -INF                      # masked where the teacher names nothing
+    g[1] = -INF                               # nothing allowed
+    index[2] = -1                             # no entry
+    value[3, 1:] = -INF                       # entries of no weight
+    mask = np.ones(n, bool)
+    mask[index[4]] = False
+    g[4, torch.from_numpy(mask).cuda()] = -INF   # the student has nothing outside the entries
+    g[5, int(index[5, 0])] = -INF             # no student mass where the teacher has some: loss infinite
+    x = g.double().cpu().numpy()
+    with np.errstate(divide="ignore"):
+        check_distill(B, g, x, value, index, None, lse if rest else None, "f32", "f32")
+    loss, grad = B.distill_grad(g, torch.from_numpy(value.astype(np.float32)).cuda(), torch.from_numpy(index).cuda(),
+                                teacher_lse=torch.from_numpy(lse).cuda() if rest else None)
+    assert loss[1] == 0 and not grad[1].any() and loss[2] == 0 and not grad[2].any()
+    assert loss[5] == INF and torch.isfinite(grad).all() and (grad[0, outside] == 0).all()
+
+
+@pytest.mark.parametrize("n", [30, 1500, 80_000])
+def test_rows_of_weight_zero_are_not_read_and_nan_stays_in_its_row(B, n):
+    rng = np.random.default_rng(n)
+    g, x = table(rng, 4, n, "f32")
+    value, index, lse = entries(rng, x, 5, "f32", short=0.0)
+    clean = B.distill_grad(g, torch.from_numpy(value.astype(np.float32)).cuda(), torch.from_numpy(index).cuda())
+    g[1] = math.nan
+    g[2, n // 2] = math.nan
+    weight = torch.tensor([1.0, 0.0, 1.0, 1.0], device="cuda")
+    loss, grad = B.distill_grad(g, torch.from_numpy(value.astype(np.float32)).cuda(), torch.from_numpy(index).cuda(),
+                                weight=weight)
+    assert loss[1] == 0 and not grad[1].any()
+    assert torch.isnan(loss[2]) and torch.isnan(grad[2]).all()
+    for r in (0, 3):
+        assert loss[r] == clean[0][r] and torch.equal(grad[r], clean[1][r])
+    g[2] = g[0]
+    g[2, 3] = INF
+    loss, grad = B.distill_grad(g, torch.from_numpy(value.astype(np.float32)).cuda(), torch.from_numpy(index).cuda(),
+                                weight=weight)
+    assert torch.isnan(loss[2]) and torch.isnan(grad[2]).all()
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,n,k", [(2, 30, 6), (2, 300, 20)])
+def test_distillation_gradient_against_differences(B, rows, n, k, rest):
+    """The gradient is the slope of the 64-bit loss: central differences with step h, whose error is h^2 / 6 of a
+    third derivative of at most 2 / ts^3 and 2^-50 / h of rounding."""
+    rng = np.random.default_rng(9)
+    g, x = table(rng, rows, n, "f32")
+    value, index, lse = entries(rng, x, k, "f32", short=0.0)
+    value = value.astype(np.float32).astype(np.float64)
+    _, grad = B.distill_grad(g, torch.from_numpy(value.astype(np.float32)).cuda(), torch.from_numpy(index).cuda(),
+                             teacher_lse=torch.from_numpy(lse).cuda() if rest else None, student_temperature=1.1,
+                             teacher_temperature=0.9)
+    grad, h = grad.double().cpu().numpy(), 1e-4
+    for r in range(rows):
+        slack = ref.distill(x[r], value[r], index[r], 1.0, float(lse[r]) if rest else None, 1.1, 0.9)[3]
+        for i in range(n):
+            ends = []
+            for sign in (1, -1):
+                y = x[r].copy()
+                y[i] += sign * h
+                ends.append(ref.distill(y, value[r], index[r], 1.0, float(lse[r]) if rest else None, 1.1, 0.9)[0])
+            slope = (ends[0] - ends[1]) / (2 * h)
+            assert abs(grad[r, i] - slope) <= h * h / 2 + 2.0 ** -46 / h + slack[i] + 2.0 ** -22 * abs(slope), (r, i)
+
+
+# ------------------------------------------------------------------------------------- as called
+def test_nothing_is_done_for_no_rows(B):
+    x = torch.empty((0, 30), device="cuda")
+    index, logp = B.choose_actions(x, torch.empty(0, device="cuda"))
+    assert len(index) == 0
+    values, index, lse = B.top_actions(x, 4)
+    assert values.shape == (0, 4)
+    loss, grad = B.distill_grad(x, values, index)
+    assert grad.shape == (0, 30) and len(loss) == 0
+
+
+def test_rows_and_columns_beside_the_given_ones_are_left_as_they_were(B):
+    rng = np.random.default_rng(2)
+    for dtype in ("f32", "bf16"):
+        for rows, n, k in ((5, 30, 4), (3, 777, 9), (2, 40_001, 33)):
+            wide, _ = table(rng, rows + 2, n + 7, dtype)
+            before = wide.clone()
+            g = wide[1:-1, 3:n + 3]
+            value, index, lse = B.top_actions(g, k)
+            out = torch.full((rows + 2, n + 7), 5.0, dtype=DT[dtype], device="cuda")
+            B.distill_grad(g, value, index, teacher_lse=lse, out=(torch.empty(rows, device="cuda"), out[1:-1, 3:n + 3]))
+            assert torch.equal(wide, before)
+            out[1:-1, 3:n + 3] = 5.0
+            assert (out == 5.0).all()
+            B.distill_grad(g, value, index, teacher_lse=lse, out=(torch.empty(rows, device="cuda"), g))
+            wide[1:-1, 3:n + 3] = before[1:-1, 3:n + 3]
+            assert torch.equal(wide, before)
+
+
+def test_teacher_to_student_to_choice_captured_and_replayed(B):
+    """A teacher's top actions distilled into a student and an action drawn from it, as one graph on a stream of
+    its own, replayed over changing inputs with eager work in between, against eager calls."""
+    torch.manual_seed(0)
+    for rows, n, k, dtype in ((64, 30, 6, "f32"), (3, 60_001, 100, "bf16"), (300, 2001, 20, "f32")):
+        teacher = torch.randn((rows, n), device="cuda").to(DT[dtype])
+        student = torch.randn((rows, n), device="cuda").to(DT[dtype])
+        u = torch.rand(rows, device="cuda")
+
+        def calls(stream=None):
+            value, index, lse = B.top_actions(teacher, k, temperature=0.5, stream=stream)
+            loss, grad = B.distill_grad(student, value, index, teacher_lse=lse, teacher_temperature=0.5, stream=stream)
+            act, logp = B.choose_actions(student, u, top_k=n // 2, top_p=0.9, stream=stream)
+            act2, logp2 = B.choose_actions(student, u, temperature=0.8, stream=stream)
+            return value, index, lse, loss, grad, act, logp, act2, logp2
+
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = calls()
+        for _ in range(4):
+            teacher.copy_(torch.randn((rows, n), device="cuda"))
+            student.copy_(torch.randn((rows, n), device="cuda"))
+            u.copy_(torch.rand(rows, device="cuda"))
+            graph.replay()
+            torch.cuda.synchronize()
+            kept = [t.clone() for t in got]
+            want = calls()
+            side.wait_stream(torch.cuda.current_stream())
+            other = calls(side)
+            torch.cuda.synchronize()
+            for a, b, c in zip(kept, want, other):
+                assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_two_streams_at_once_do_not_disturb_each_other(B):
+    torch.manual_seed(1)
+    xs = [torch.randn((2, 90_000 + 100 * i), device="cuda") for i in range(2)]
+    us = [torch.rand(2, device="cuda") for _ in range(2)]
+    calls = lambda i, s: (*B.choose_actions(xs[i], us[i], top_p=0.9, stream=s), *B.top_actions(xs[i], 200, stream=s))
+    want = [calls(i, None) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [calls(i, streams[i]) for i in range(2)]
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_the_same_call_gives_the_same_bits(B):
+    torch.manual_seed(2)
+    for rows, n, k in ((300, 5000, 200), (2, 131_072, 700)):
+        x = torch.randn((rows, n), device="cuda")
+        u = torch.rand(rows, device="cuda")
+        value, index, lse = B.top_actions(x, k)
+        y = torch.randn((rows, n), device="cuda")
+        calls = lambda: (*B.choose_actions(x, u, top_p=0.9), *B.choose_actions(x, u), *B.top_actions(x, k),
+                         *B.distill_grad(y, value, index, teacher_lse=lse))
+        want = calls()
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(calls(), want))
+
+
+def test_a_table_beyond_4_gib(B):
+    """Offsets of the last rows pass 32 bits, in elements and in bytes."""
+    n = 262_144
+    rows = (1 << 32) // n + 3
+    x = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+    x.normal_()
+    u = torch.rand(rows, device="cuda")
+    index, logp = B.choose_actions(x, u, top_k=20)
+    i2, l2 = B.choose_actions(x, u, top_p=0.8)
+    value, top, lse = B.top_actions(x, 16)
+    last = slice(rows - 3, rows)
+    few = x[last].clone()
+    for how, got in (({"top_k": 20}, index), ({"top_p": 0.8}, i2)):
+        assert torch.equal(B.choose_actions(few, u[last].clone(), **how)[0], got[last])
+    check_choice(few.double().cpu().numpy(), u[last].cpu().numpy(), {"top_k": 20}, index[last], logp[last])
+    check_choice(few.double().cpu().numpy(), u[last].cpu().numpy(), {"top_p": 0.8}, i2[last], l2[last])
+    check_top(few.double().cpu().numpy(), 16, 1.0, value[last], top[last], lse[last])
+    loss, grad = B.distill_grad(x, value, top, teacher_lse=lse, student_temperature=2.0)
+    a, b = B.distill_grad(few, value[last].clone(), top[last].clone(), teacher_lse=lse[last].clone(), student_temperature=2.0)
+    assert torch.equal(loss[last], a) and torch.equal(grad[last], b)

@@ -20,6 +20,7 @@ struct TopArgs {
     LogitRows x;
     unsigned int k;
     double inv_t;
+    float c2;             // log2(e) / temperature
     unsigned char* values;
     int* index;
     float* lse;
@@ -47,6 +48,7 @@ __device__ void search_sum(const T* x, unsigned int n, float m, double inv_t, In
                            unsigned long long* mass, unsigned int* count) {
     unsigned long long a = 0;
     unsigned int c = 0;
+#pragma unroll 1
     for (unsigned int i = threadIdx.x; i < n; i += 64 * W) {
         const float v = clean_logit(logit_value(x + i));
         if (!in(order_key(v)) || v == -INFINITY) continue;
@@ -64,6 +66,7 @@ template <int W, typename T>
 __device__ unsigned int search_equal(const T* x, unsigned int n, unsigned int v, unsigned int c, SearchShared<W>& s) {
     const unsigned int lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     unsigned int found = 0xFFFFFFFFu, before = 0;
+#pragma unroll 1
     for (unsigned int i0 = 0; i0 < n; i0 += 64 * W) {
         const unsigned int i = i0 + threadIdx.x;
         const bool hit = i < n && order_key(clean_logit(logit_value(x + i))) == v;
@@ -89,6 +92,7 @@ __device__ unsigned int search_equal(const T* x, unsigned int n, unsigned int v,
 // The largest key v in [lo, hi] whose logits and those above it satisfy `enough` (monotone in v; the lowest does).
 template <int W, typename Enough>
 __device__ unsigned int search_key(unsigned int lo, unsigned int hi, Enough enough) {
+#pragma unroll 1
     while (lo < hi) {
         const unsigned int mid = lo + (hi - lo) / 2u + ((hi - lo) & 1u);
         if (enough(mid)) lo = mid;
@@ -104,6 +108,7 @@ __device__ void choose_by_search(const ChooseArgs& p, unsigned long long row, Se
     unsigned int turn = 0;
     // the allowed logits' range and number
     unsigned int hi = kMaskedKey, lo = 0xFFFFFFFFu, allowed = 0;
+#pragma unroll 1
     for (unsigned int i = threadIdx.x; i < n; i += 64 * W) {
         const float v = clean_logit(logit_value(x + i));
         if (v == -INFINITY) continue;
@@ -190,25 +195,65 @@ __device__ void choose_by_search(const ChooseArgs& p, unsigned long long row, Se
     }
 }
 
-template <int W, typename T>
-__global__ __launch_bounds__(64 * W) void choose_search_kernel(ChooseArgs p) {
-    __shared__ SearchShared<W> s;
-    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
-        choose_by_search<W, T>(p, row, s);
-        __syncthreads();
-    }
-}
 
 __device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_value(unsigned short* p, float v) { *p = (unsigned short)(__float_as_uint(v) >> 16); }
 
-// Sorts `count` (a power of two) numbers in LDS, the largest first.
+// ------------------------------------------------------------------- one workgroup per row, by candidates
+constexpr unsigned int kBins = 2048;    // of the histogram of weights
+constexpr unsigned int kList = 2048;    // actions that are sorted in LDS
+constexpr unsigned int kSliceBins = 1024;
+
+template <int W>
+struct ChooseShared {
+    union {
+        unsigned long long hist[kBins];     // 2^-44 of the weight at the bin's middle
+        double sums[kBins];                 // inclusive sums over bins, or over a sorted list
+        unsigned int slices[kSliceBins];
+    };
+    unsigned long long words[kList];
+    SearchShared<W> search;
+    double part[W];
+    unsigned int taken, bin;
+    float key;
+};
+
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Sorts `count` numbers in LDS (room for the next power of two), the largest first.  Up to 128: every
+// thread ranks one against all.  More: a bitonic network, where exchanges over less than 128 places stay within
+// the 128 numbers of one wavefront and need no barrier.
 template <int W>
 __device__ void sort_words(unsigned long long* w, unsigned int count) {
-    for (unsigned int size = 2; size <= count; size <<= 1)
+    const unsigned int tid = threadIdx.x;
+    if (count <= 128u) {
+        unsigned long long mine = 0;
+        unsigned int rank = 0;
+        __syncthreads();
+        if (tid < count) {
+            mine = w[tid];
+#pragma unroll 4
+            for (unsigned int j = 0; j < count; ++j) rank += w[j] > mine;
+        }
+        __syncthreads();
+        if (tid < count) w[rank] = mine;
+        __syncthreads();
+        return;
+    }
+    unsigned int padded = 256;
+    while (padded < count) padded <<= 1;
+    for (unsigned int i = count + tid; i < padded; i += 64 * W) w[i] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (unsigned int size = 2; size <= padded; size <<= 1)
+#pragma unroll 1
         for (unsigned int gap = size >> 1; gap; gap >>= 1) {
-            __syncthreads();
-            for (unsigned int t = threadIdx.x; t < count / 2u; t += 64 * W) {
+#pragma unroll 1
+            for (unsigned int t = tid; t < padded / 2u; t += 64 * W) {
                 const unsigned int i = 2u * t - (t & (gap - 1u)), j = i + gap;
                 const unsigned long long a = w[i], b = w[j];
                 if ((a < b) == ((i & size) == 0)) {
@@ -216,86 +261,665 @@ __device__ void sort_words(unsigned long long* w, unsigned int count) {
                     w[j] = a;
                 }
             }
+            // (the next exchange is over gap / 2, or over `size` after the last of this size)
+            if (gap >= 128u || (gap == 1u && size >= 128u)) __syncthreads();
+            else wave_lds_fence();
         }
     __syncthreads();
 }
 
-template <int W, typename T>
-__global__ __launch_bounds__(64 * W) void top_search_kernel(TopArgs p) {
-    __shared__ SearchShared<W> s;
-    __shared__ unsigned long long words[kMaxTop];
-    __shared__ unsigned int taken;
-    __shared__ double part[2][W];
-    const unsigned int n = p.x.n;
-    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
-        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
-        unsigned int turn = 0, hi = kMaskedKey, allowed = 0;
-        for (unsigned int i = threadIdx.x; i < n; i += 64 * W) {
-            const unsigned int k = order_key(clean_logit(logit_value(x + i)));
-            hi = max(hi, k);
-            allowed += k > kMaskedKey;
+// The elements that `in` takes, as words in LDS in any order; returns their number, which may pass kList (the
+// rest is not kept then).
+template <int W, typename Row, typename In>
+__device__ unsigned int gather_words(const Row& row, ChooseShared<W>& s, In in) {
+    if (threadIdx.x == 0) s.taken = 0;
+    __syncthreads();
+    row.each([&](float x, unsigned int i, int) {
+        if (in(x)) {
+            const unsigned int at = atomicAdd(&s.taken, 1u);
+            if (at < kList) s.words[at] = order_word(logit_key(x), i);
         }
-        __syncthreads();
-        hi = block_reduce<W>(hi, MaxOp{}, s.count[0]);
-        allowed = block_reduce<W>(allowed, SumOp{}, s.count[1]);
-        __syncthreads();
-        const float m = key_value(hi);
-        if (p.lse) {
-            double a = 0.0;
-            if (allowed)
-                for (unsigned int i = threadIdx.x; i < n; i += 64 * W) {
-                    const float v = clean_logit(logit_value(x + i));
-                    if (v != -INFINITY) a += exp(-logit_depth(m, v, p.inv_t));
-                }
-            a = block_reduce<W>(a, SumOp{}, part[0]);
-            if (threadIdx.x == 0) p.lse[row] = allowed ? (float)((double)m * p.inv_t + log(a)) : -INFINITY;
-        }
-        const unsigned int k = min(p.k, allowed);
-        unsigned int v = 0, above = 0;
-        if (k) {
-            v = search_key<W>(kMaskedKey + 1u, hi, [&](unsigned int v) {
-                unsigned int c;
-                search_sum<W>(x, n, m, 0.0, [&](unsigned int key) { return key >= v; }, s, turn, nullptr, &c);
-                return c >= k;
-            });
-            search_sum<W>(x, n, m, 0.0, [&](unsigned int key) { return key > v; }, s, turn, nullptr, &above);
-        }
-        // the logits above v in any order, then the first k - above equal to it
-        for (unsigned int i = threadIdx.x; i < kMaxTop; i += 64 * W) words[i] = 0;
-        if (threadIdx.x == 0) taken = 0;
-        __syncthreads();
-        const unsigned int lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-        unsigned int equal_before = 0;
-        if (k)
-            for (unsigned int i0 = 0; i0 < n; i0 += 64 * W) {
-                const unsigned int i = i0 + threadIdx.x;
-                const unsigned int key = i < n ? order_key(clean_logit(logit_value(x + i))) : 0u;
-                if (key > v) words[atomicAdd(&taken, 1u)] = order_word(key, i);
-                const unsigned long long hits = __ballot(key == v);
-                __syncthreads();
-                if (lane == 0) s.count[0][wave] = __popcll(hits);
-                __syncthreads();
-                unsigned int at = equal_before + __popcll(hits & ((1ull << lane) - 1ull));
-                for (unsigned int w = 0; w < W; ++w) {
-                    if (w < wave) at += s.count[0][w];
-                    equal_before += s.count[0][w];
-                }
-                if (key == v && above + at < k) words[above + at] = order_word(key, i);
+    });
+    __syncthreads();
+    const unsigned int taken = s.taken;
+    __syncthreads();
+    return taken;
+}
+
+template <int W, typename Row>
+__device__ float row_max(const Row& row, ChooseShared<W>& s) {
+    float m = -INFINITY;
+    row.each([&](float x, unsigned int, int) { m = fmaxf(m, x); });
+    m = wave_reduce(m, MaxOp{});
+    float* part = reinterpret_cast<float*>(s.part);
+    __syncthreads();
+    if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, part[w]);
+    __syncthreads();
+    return m + 0.f;
+}
+
+// Number of the first of `bins` counts at which their running sum reaches `need` (the last one if it never does).
+// Called by one wavefront.
+__device__ __forceinline__ unsigned int bin_of_count(const unsigned int* counts, unsigned int bins, unsigned int need) {
+    const unsigned int lane = threadIdx.x & 63u, per = bins / 64u;
+    unsigned int mine = 0;
+    for (unsigned int j = 0; j < per; ++j) mine += counts[lane * per + j];
+    unsigned int upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const unsigned int o = __shfl_up(upto, off, 64);
+        if (lane >= (unsigned int)off) upto += o;
+    }
+    const unsigned long long there = __ballot(upto >= need);
+    if (!there) return bins - 1u;
+    const unsigned int owner = __ffsll((long long)there) - 1u;
+    unsigned int bin = 0, run = upto - mine;
+    if (lane == owner)
+        for (unsigned int j = 0; j < per; ++j) {
+            run += counts[lane * per + j];
+            if (run >= need) {
+                bin = lane * per + j;
+                break;
             }
-        unsigned int padded = 2;
-        while (padded < p.k) padded <<= 1;
-        sort_words<W>(words, padded);
-        for (unsigned int j = threadIdx.x; j < p.k; j += 64 * W) {
-            const unsigned long long at = row * p.k + j;
-            store_value(reinterpret_cast<T*>(p.values) + at, j < k ? key_value(word_key(words[j])) : -INFINITY);
-            p.index[at] = j < k ? (int)word_index(words[j]) : -1;
         }
+    return __shfl(bin, (int)owner, 64);
+}
+
+// A value that the k largest of a row (maximum m) are not below, and not many more are not: the k-th largest of
+// the slices' maxima, to one of 1024 steps.  A slice is what a thread holds in one place of its loads, so the slices
+// are 64 W times 4 or 8, at least 1024.
+template <int W, int SLOTS>
+__device__ float top_threshold(const float (&slot)[SLOTS], float m, unsigned int k, ChooseShared<W>& s) {
+    const unsigned int tid = threadIdx.x;
+    float low = INFINITY;
+#pragma unroll
+    for (int e = 0; e < SLOTS; ++e)
+        if (slot[e] > -INFINITY) low = fminf(low, slot[e]);
+    low = wave_reduce(low, MinOp{});
+    float* part = reinterpret_cast<float*>(s.part);
+    __syncthreads();
+    if ((tid & 63u) == 0) part[tid >> 6] = low;
+    for (unsigned int i = tid; i < kSliceBins; i += 64 * W) s.slices[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) low = fminf(low, part[w]);
+    const float range = m - low;
+    const float scale = range > 0.f && range < INFINITY ? (kSliceBins - 1) / range : 0.f;
+#pragma unroll
+    for (int e = 0; e < SLOTS; ++e)
+        if (slot[e] > -INFINITY)
+            atomicAdd(&s.slices[min((unsigned int)((m - slot[e]) * scale), kSliceBins - 1u)], 1u);
+    __syncthreads();
+    if (tid < 64) {
+        const unsigned int b = bin_of_count(s.slices, kSliceBins, k);
+        // (the lower edge, and a little more than its rounding can be off; the last bin takes all that is allowed)
+        if (tid == 0) {
+            const float t = m - (float)(b + 1u) * (range / (kSliceBins - 1)) * 1.00001f;
+            s.key = b + 1u == kSliceBins ? -3.402823466e38f
+                    : range == 0.f      ? m
+                    : scale > 0.f       ? t - fabsf(t) * 0x1p-22f
+                                        : -3.402823466e38f;
+        }
+    }
+    __syncthreads();
+    return s.key;
+}
+
+// The first k and perhaps more of the row, sorted; returns how many, or more than kList if they do not fit.
+template <int W, int SLOTS, typename Row>
+__device__ unsigned int top_words(const Row& row, float m, unsigned int k, ChooseShared<W>& s) {
+    float slot[SLOTS];
+#pragma unroll
+    for (int e = 0; e < SLOTS; ++e) slot[e] = -INFINITY;
+    row.each([&](float x, unsigned int, int e) { slot[e] = fmaxf(slot[e], x); });
+    const float t = top_threshold<W, SLOTS>(slot, m, k, s);
+    return gather_words<W>(row, s, [&](float x) { return x >= t; });
+}
+
+// ---------------------------------------------------------------------------------- sums along a sorted list
+// Inclusive sums of the weights of words[0 .. count) behind `before`, into sums[].  Called by one wavefront.
+__device__ __forceinline__ void list_sums(const unsigned long long* words, unsigned int count, double before, float m,
+                                          double inv_t, double* sums) {
+    const unsigned int lane = threadIdx.x & 63u;
+#pragma unroll 1
+    for (unsigned int j0 = 0; j0 < count; j0 += 64) {
+        const unsigned int j = j0 + lane;
+        double c = j < count ? exp(-logit_depth(m, key_value(word_key(words[j])), inv_t)) : 0.0;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const double o = __shfl_up(c, off, 64);
+            if (lane >= (unsigned int)off) c += o;
+        }
+        c += before;
+        if (j < count) sums[j] = c;
+        before = __shfl(c, 63, 64);
+    }
+}
+// How many of the sums `low` holds for: the sums rise, so they are the first ones.  Called by one wavefront.
+template <typename Low>
+__device__ __forceinline__ unsigned int list_count(unsigned int count, Low low) {
+    unsigned int n = 0;
+#pragma unroll 1
+    for (unsigned int j0 = 0; j0 < count; j0 += 64) {
+        const unsigned int j = j0 + (threadIdx.x & 63u);
+        const unsigned int here = __popcll(__ballot(j < count && low(j)));
+        n += here;
+        if (here < 64u) break;
+    }
+    return n;
+}
+
+struct RowChoice {
+    double inv_t, top_p, min_p;
+    float u;
+    unsigned int k;      // 1 .. 1024: so many; 0: all
+    bool greedy, search; // search: more than 1024
+};
+__device__ __forceinline__ RowChoice row_choice(const ChooseArgs& p, unsigned long long row) {
+    RowChoice c;
+    const double t = p.row_temperature ? (double)p.row_temperature[row] : p.temperature;
+    const long long k = p.row_top_k ? (long long)p.row_top_k[row] : p.top_k;
+    c.top_p = p.row_top_p ? (double)p.row_top_p[row] : p.top_p;
+    c.min_p = p.row_min_p ? (double)p.row_min_p[row] : p.min_p;
+    c.u = p.u[row];
+    c.greedy = !(t > 0.0);
+    // (beyond these ends the temperature changes no float's weight, and products with it stay finite)
+    c.inv_t = c.greedy ? 1.0 : 1.0 / fmin(fmax(t, 1e-250), 1e250);
+    c.search = false;
+    c.k = c.greedy ? 1u : 0u;
+    if (!c.greedy && k > 0 && k < (long long)p.x.n) {
+        c.k = k <= (long long)kMaxTop ? (unsigned int)k : 0u;
+        c.search = c.k == 0u;
+    }
+    return c;
+}
+
+__device__ __forceinline__ void put_choice(const ChooseArgs& p, unsigned long long row, int index, float logp) {
+    p.index[row] = index;
+    if (p.logp) p.logp[row] = logp;
+}
+
+// The choice from the row's sorted first actions (at least min(k, allowed) of them).  Called by one wavefront.
+__device__ void choose_from_list(const ChooseArgs& p, unsigned long long row, const RowChoice& c,
+                                 const unsigned long long* words, unsigned int count, float m, double* sums) {
+    const unsigned int lane = threadIdx.x & 63u;
+    if (c.greedy) {
+        if (lane == 0) put_choice(p, row, (int)word_index(words[0]), 0.f);
+        return;
+    }
+    count = min(count, c.k);
+    list_sums(words, count, 0.0, m, c.inv_t, sums);
+    wave_lds_fence();
+    unsigned int left = count;
+    if (c.top_p < 1.0) {
+        const double most = c.top_p * sums[count - 1u];
+        left = list_count(count - 1u, [&](unsigned int j) { return sums[j] < most; }) + 1u;
+    }
+    if (c.min_p > 0.0) {
+        const unsigned int n = list_count(
+            left, [&](unsigned int j) { return exp(-logit_depth(m, key_value(word_key(words[j])), c.inv_t)) >= c.min_p; });
+        left = n ? n : 1u;
+    }
+    const double mass = sums[left - 1u], drawn = c.u > 0.f ? (double)c.u * mass : 0.0;
+    const unsigned int at = min(list_count(left, [&](unsigned int j) { return sums[j] <= drawn; }), left - 1u);
+    if (lane == 0)
+        put_choice(p, row, (int)word_index(words[at]),
+                   (float)(-logit_depth(m, key_value(word_key(words[at])), c.inv_t) - log(mass)));
+}
+
+// ------------------------------------------------------------------------------- the histogram of a row's weights
+// Bins are as wide as a power of two near temperature / 32 and aligned to its multiples: x / width, its whole part and
+// what is left are exact in 64 bits, and pieces of a row can be binned on their own.  2048 bins reach
+// 40 temperatures below the maximum or further; what lies below has less than 2^18 e^-40 = 1.2e-12 of the best action's
+// weight together, where a random number of 24 bits cannot fall.
+struct Bins {
+    double width, inv_width, slope;   // slope: width / temperature
+    double top;                       // number of the maximum's bin, counted from value 0
+    __device__ __forceinline__ Bins(float m, double inv_t) {
+        // 40 / 2048 = 0.0195 temperatures, rounded up to a power of two
+        int e;
+        (void)frexp((40.0 / kBins) / inv_t, &e);
+        width = ldexp(1.0, e);
+        inv_width = ldexp(1.0, -e);
+        slope = width * inv_t;
+        top = floor((double)m * inv_width);
+    }
+    // the floats of bin b are lo <= x < hi
+    __device__ __forceinline__ float lo(double b) const { return __double2float_ru((top - b) * width); }
+    // (nothing is above bin 0; where logits are so large that top + 1 is top, it holds the maximum alone)
+    __device__ __forceinline__ float hi(double b) const {
+        return b == 0.0 ? INFINITY : __double2float_ru((top - b + 1.0) * width);
+    }
+    // weight at the middle of bin b
+    __device__ __forceinline__ double middle(float m, double b) const {
+        return exp(-((double)m * inv_width - (top - b) - 0.5) * slope);
+    }
+};
+
+template <int W, typename Row>
+__device__ void bin_weights(const Row& row, const Bins& bins, ChooseShared<W>& s) {
+    for (unsigned int i = threadIdx.x; i < kBins; i += 64 * W) s.hist[i] = 0;
+    __syncthreads();
+    const float least = bins.lo((double)(kBins - 1));
+    const double inv_width = bins.inv_width, slope = bins.slope, top = bins.top;
+    row.each([&](float x, unsigned int, int) {
+        if (x >= least) {
+            const double at = (double)x * inv_width, whole = floor(at);
+            // exp of a number within +- 0.0195: the sixth power's term, which is left out, is below 2^-43
+            const double z = fma(at - whole, slope, -0.5 * slope);
+            double w = fma(z, 1.0 / 120.0, 1.0 / 24.0);
+            w = fma(w, z, 1.0 / 6.0);
+            w = fma(w, z, 0.5);
+            w = fma(w, z, 1.0);
+            w = fma(w, z, 1.0);
+            // (adding 2^52 leaves the whole number in the low bits)
+            const unsigned long long units = __double_as_longlong(fma(w, kOne, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+            atomicAdd(&s.hist[(int)(top - whole)], units);
+        }
+    });
+    __syncthreads();
+}
+
+// hist -> inclusive sums of the weights (the best action's is 1), in place.
+template <int W>
+__device__ void sum_bins(const Bins& bins, float m, ChooseShared<W>& s) {
+    constexpr int kPer = kBins / (64 * W);
+    const unsigned int tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    double c[kPer], run = 0.0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const unsigned int b = tid * kPer + j;
+        const unsigned long long h = s.hist[b];
+        if (h) run += (double)h * (1.0 / kOne) * bins.middle(m, (double)b);
+        c[j] = run;
+    }
+    double upto = run;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const double o = __shfl_up(upto, off, 64);
+        if (lane >= (unsigned int)off) upto += o;
+    }
+    __syncthreads();
+    if (lane == 63u) s.part[wave] = upto;
+    __syncthreads();
+    double base = 0.0, before = __shfl_up(upto, 1, 64);
+    if (lane == 0) before = 0.0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) base += (unsigned int)w < wave ? s.part[w] : 0.0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) s.sums[tid * kPer + j] = base + (before + c[j]);
+    __syncthreads();
+}
+
+// The first bin whose inclusive sum `reached` holds for; kBins - 1 if none.  (Neighbouring sums are made in
+// different orders and may fall by a last bit where they should rise: the lowest such bin counts.)
+template <int W, typename Reached>
+__device__ unsigned int find_bin(ChooseShared<W>& s, Reached reached) {
+    constexpr int kPer = kBins / (64 * W);
+    if (threadIdx.x == 0) s.bin = kBins - 1;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const unsigned int b = threadIdx.x * kPer + j;
+        if (reached(s.sums[b]) && (b == 0 || !reached(s.sums[b - 1u]))) atomicMin(&s.bin, b);
+    }
+    __syncthreads();
+    const unsigned int bin = s.bin;
+    __syncthreads();
+    return bin;
+}
+
+// From the inclusive sums over bins to the choice; false if a bin holds too many actions to be sorted.
+template <int W, typename Row>
+__device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned long long row, const RowChoice& c,
+                                 const Bins& bins, float m, ChooseShared<W>& s) {
+    const unsigned int tid = threadIdx.x;
+    double mass = s.sums[kBins - 1];
+    unsigned int have = kBins, count = 0, limit = 0xFFFFFFFFu;   // the bin whose sorted actions are in LDS, their number
+    auto list_bin = [&](unsigned int b) {
+        const float lo = bins.lo((double)b), hi = bins.hi((double)b);
+        count = gather_words<W>(row_, s, [&](float x) { return x >= lo && x < hi; });
+        if (count > kList) return false;
+        sort_words<W>(s.words, count);
+        have = b;
+        return true;
+    };
+    // the sum over the actions that stay
+    unsigned int last = kBins - 1;
+    const bool cut_p = c.top_p < 1.0, cut_m = c.min_p > 0.0;
+    if (cut_p || cut_m) {
+        unsigned int bin_p = kBins, bin_m = kBins;
+        // (the best action always stays, and the sum reaches its weight with it)
+        const double most = fmax(c.top_p * mass, 0.5);
+        if (cut_p) bin_p = find_bin<W>(s, [&](double v) { return v >= most; });
+        if (cut_m) {
+            const double b = bins.top - floor(((double)m + log(fmin(c.min_p, 1.0)) / c.inv_t) * bins.inv_width);
+            bin_m = b < (double)kBins ? (unsigned int)fmax(b, 0.0) : kBins;
+        }
+        last = min(bin_p, bin_m);
+        if (last < kBins) {
+            if (!list_bin(last)) return false;
+            const double before = last ? s.sums[last - 1u] : 0.0;
+            __syncthreads();
+            if (tid < 64) {
+                // walk the list 64 at a time: how many stay, and their sum
+                double run = before, kept = before;
+                unsigned int n = 0;
+#pragma unroll 1
+                for (unsigned int j0 = 0; j0 < count; j0 += 64) {
+                    const unsigned int j = j0 + tid;
+                    const double w = j < count ? exp(-logit_depth(m, key_value(word_key(s.words[j])), c.inv_t)) : 0.0;
+                    double v = w;
+#pragma unroll
+                    for (int off = 1; off < 64; off <<= 1) {
+                        const double o = __shfl_up(v, off, 64);
+                        if (tid >= (unsigned int)off) v += o;
+                    }
+                    v += run;
+                    double prev = __shfl_up(v, 1, 64);
+                    if (tid == 0) prev = run;
+                    bool stays = j < count && (!cut_p || bin_p > last || prev < most) && (!cut_m || bin_m > last || w >= c.min_p);
+                    if (last == 0 && j == 0) stays = true;
+                    const unsigned long long yes = __ballot(stays);
+                    const unsigned int here = __popcll(yes);
+                    if (here) kept = __shfl(v, (int)here - 1, 64);
+                    n += here;
+                    run = __shfl(v, 63, 64);
+                    if (here < 64u) break;
+                }
+                if (tid == 0) {
+                    s.part[0] = kept;
+                    s.taken = n;
+                }
+            }
+            __syncthreads();
+            mass = s.part[0];
+            limit = s.taken;
+            __syncthreads();
+        }
+    }
+    // (nothing of the last bin may stay: the choice then lies in one before it)
+    const bool end = !(c.u < 1.f);
+    const double drawn = end ? mass : c.u > 0.f ? (double)c.u * mass : 0.0;
+    const unsigned int bin = min(find_bin<W>(s, [&](double v) { return end ? v >= drawn : v > drawn; }), last);
+    if (bin != have && !list_bin(bin)) return false;
+    const double before = bin ? s.sums[bin - 1u] : 0.0;
+    if (tid < 64) {
+        const unsigned int n = bin == last ? min(count, limit) : count;
+        double run = before;
+        unsigned int at = n ? n - 1u : 0u;
+#pragma unroll 1
+        for (unsigned int j0 = 0; j0 < n; j0 += 64) {
+            const unsigned int j = j0 + tid;
+            double v = j < n ? exp(-logit_depth(m, key_value(word_key(s.words[j])), c.inv_t)) : 0.0;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const double o = __shfl_up(v, off, 64);
+                if (tid >= (unsigned int)off) v += o;
+            }
+            v += run;
+            const unsigned long long yes = __ballot(j < n && (end ? v >= drawn : v > drawn));
+            if (yes) {
+                at = j0 + __ffsll((long long)yes) - 1u;
+                break;
+            }
+            run = __shfl(v, 63, 64);
+        }
+        if (tid == 0)
+            put_choice(p, row, (int)word_index(s.words[at]),
+                       (float)(-logit_depth(m, key_value(word_key(s.words[at])), c.inv_t) - log(mass)));
+    }
+    return true;
+}
+
+// One row, all of it at hand.
+template <int W, int SLOTS, typename T, typename Row>
+__device__ void choose_row(const Row& held, const ChooseArgs& p, unsigned long long row, ChooseShared<W>& s) {
+    const RowChoice c = row_choice(p, row);
+    const float m = row_max<W>(held, s);
+    if (m == -INFINITY) {
+        if (threadIdx.x == 0) put_choice(p, row, -1, 0.f);
+        return;
+    }
+    bool done = false;
+    if (!c.search && !(m == INFINITY)) {
+        if (c.k) {
+            const unsigned int count = top_words<W, SLOTS>(held, m, c.k, s);
+            if (count <= kList) {
+                sort_words<W>(s.words, count);
+                if (threadIdx.x < 64) choose_from_list(p, row, c, s.words, count, m, s.sums);
+                done = true;
+            }
+        } else {
+            const Bins bins(m, c.inv_t);
+            bin_weights<W>(held, bins, s);
+            sum_bins<W>(bins, m, s);
+            done = choose_from_bins<W>(held, p, row, c, bins, m, s);
+        }
+    }
+    if (!done) {
         __syncthreads();
+        choose_by_search<W, T>(p, row, s.search);
     }
 }
 
-// Workgroups of one launch: a row each, more rows than that in turn.
+template <int W, int NV, typename T>
+__global__ __launch_bounds__(64 * W) void choose_kernel(ChooseArgs p) {
+    __shared__ ChooseShared<W> s;
+    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
+        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        __syncthreads();
+        if constexpr (NV > 0) {
+            const HeldRow<W, NV, T> held(x, 0, p.x.n);
+            choose_row<W, (int)kPerLoad<T>, T>(held, p, row, s);
+        } else {
+            const ReadRow<W, T> read(x, 0, p.x.n);
+            choose_row<W, (int)kPerLoad<T>, T>(read, p, row, s);
+        }
+    }
+}
+
+// -------------------------------------------------------------------------------------------- top actions
+template <int W, typename T>
+__device__ void put_top(const TopArgs& p, unsigned long long row, const unsigned long long* words, unsigned int count) {
+    for (unsigned int j = threadIdx.x; j < p.k; j += 64 * W) {
+        const unsigned long long at = row * p.k + j;
+        store_value(reinterpret_cast<T*>(p.values) + at, j < count ? key_value(word_key(words[j])) : -INFINITY);
+        p.index[at] = j < count ? (int)word_index(words[j]) : -1;
+    }
+}
+
+// The first k actions by search: those above the k-th value in any order, then the first ones equal to it.
+template <int W, typename T>
+__device__ unsigned int top_by_search(const T* x, unsigned int n, unsigned int k, float m, ChooseShared<W>& s) {
+    unsigned int turn = 0, allowed, above;
+    search_sum<W>(x, n, m, 0.0, [](unsigned int) { return true; }, s.search, turn, nullptr, &allowed);
+    k = min(k, allowed);
+    const unsigned int v = search_key<W>(kMaskedKey + 1u, order_key(m), [&](unsigned int v) {
+        unsigned int c;
+        search_sum<W>(x, n, m, 0.0, [&](unsigned int key) { return key >= v; }, s.search, turn, nullptr, &c);
+        return c >= k;
+    });
+    search_sum<W>(x, n, m, 0.0, [&](unsigned int key) { return key > v; }, s.search, turn, nullptr, &above);
+    if (threadIdx.x == 0) s.taken = 0;
+    __syncthreads();
+    const unsigned int lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    unsigned int equal_before = 0;
+#pragma unroll 1
+    for (unsigned int i0 = 0; i0 < n; i0 += 64 * W) {
+        const unsigned int i = i0 + threadIdx.x;
+        const unsigned int key = i < n ? logit_key(logit_value(x + i)) : 0u;
+        if (key > v) s.words[atomicAdd(&s.taken, 1u)] = order_word(key, i);
+        const unsigned long long hits = __ballot(key == v);
+        __syncthreads();
+        if (lane == 0) s.search.count[0][wave] = __popcll(hits);
+        __syncthreads();
+        unsigned int at = equal_before + __popcll(hits & ((1ull << lane) - 1ull));
+        for (unsigned int w = 0; w < W; ++w) {
+            if (w < wave) at += s.search.count[0][w];
+            equal_before += s.search.count[0][w];
+        }
+        if (key == v && above + at < k) s.words[above + at] = order_word(key, i);
+    }
+    return k;
+}
+
+template <int W, int SLOTS, typename T, typename Row>
+__device__ void top_row(const Row& held, const TopArgs& p, unsigned long long row, const T* x, ChooseShared<W>& s) {
+    const float m = row_max<W>(held, s);
+    if (p.lse) {
+        // (the sum of a load in 32 bits, sums of those in 64)
+        double a = 0.0;
+        if (m > -INFINITY && m < INFINITY) {
+            float load = 0.f;
+            held.each([&](float v, unsigned int, int e) {
+                const float w = __builtin_amdgcn_exp2f((fmaxf(v, -INFINITY) - m) * p.c2);
+                load = e ? load + w : w;
+                if (e == SLOTS - 1) a += (double)load;
+            });
+        }
+        const double total = block_reduce<W>(a, SumOp{}, s.part);
+        if (threadIdx.x == 0)
+            p.lse[row] = m == INFINITY || m == -INFINITY ? m : (float)((double)m * p.inv_t + log(total));
+        __syncthreads();
+    }
+    unsigned int count = 0;
+    if (m > -INFINITY) {
+        count = top_words<W, SLOTS>(held, m, p.k, s);
+        if (count > kList) count = top_by_search<W, T>(x, p.x.n, p.k, m, s);
+        sort_words<W>(s.words, count);
+    }
+    put_top<W, T>(p, row, s.words, min(count, p.k));
+}
+
+template <int W, int NV, typename T>
+__global__ __launch_bounds__(64 * W) void top_kernel(TopArgs p) {
+    __shared__ ChooseShared<W> s;
+    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
+        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        __syncthreads();
+        if constexpr (NV > 0) {
+            const HeldRow<W, NV, T> held(x, 0, p.x.n);
+            top_row<W, (int)kPerLoad<T>, T>(held, p, row, x, s);
+        } else {
+            const ReadRow<W, T> read(x, 0, p.x.n);
+            top_row<W, (int)kPerLoad<T>, T>(read, p, row, x, s);
+        }
+    }
+}
+
+// ------------------------------------------------------------------- rows of up to 64 actions: one wavefront each
+__device__ __forceinline__ double lane_value(double v, int lane) {
+    const unsigned long long b = __double_as_longlong(v);
+    const unsigned int lo = __builtin_amdgcn_readlane((int)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
+    return __longlong_as_double((long long)((unsigned long long)hi << 32 | lo));
+}
+
+// Which lanes come before this one in the order of choice, a bit each.
+__device__ __forceinline__ unsigned long long lanes_before(unsigned int key, unsigned int n) {
+    const unsigned int lane = threadIdx.x & 63u;
+    unsigned long long before = 0;
+    for (unsigned int j = 0; j < n; ++j) {
+        const unsigned int other = __builtin_amdgcn_readlane((int)key, (int)j);
+        before |= (unsigned long long)(other > key || (other == key && j < lane)) << j;
+    }
+    return before;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void choose_wave_kernel(ChooseArgs p) {
+    const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
+    const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (unsigned long long row = blockIdx.x * 4ull + wave; row < p.x.rows; row += gridDim.x * 4ull) {
+        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
+        const RowChoice c = row_choice(p, row);
+        const long long k = p.row_top_k ? (long long)p.row_top_k[row] : p.top_k;
+        const unsigned long long before_me = lanes_before(order_key(v), n);
+        const unsigned int rank = __popcll(before_me);
+        const bool allowed = v > -INFINITY;
+        const float m = wave_reduce(v, MaxOp{});
+        if (m == -INFINITY) {
+            if (lane == 0) put_choice(p, row, -1, 0.f);
+            continue;
+        }
+        if (c.greedy) {
+            if (rank == 0) put_choice(p, row, (int)lane, 0.f);
+            continue;
+        }
+        const double w = allowed && (k <= 0 || (long long)rank < k) ? exp(-logit_depth(m, v, c.inv_t)) : 0.0;
+        double before = 0.0, total = 0.0;
+        for (unsigned int j = 0; j < n; ++j) {
+            const double other = lane_value(w, (int)j);
+            total += other;
+            before += before_me >> j & 1ull ? other : 0.0;
+        }
+        bool stays = w > 0.0;
+        if (c.top_p < 1.0) stays &= before < c.top_p * total;
+        if (c.min_p > 0.0) stays &= w >= c.min_p;
+        stays |= rank == 0;
+        const double upto = before + w;
+        const double mass = wave_reduce(stays ? upto : 0.0, MaxOp{});
+        const double drawn = c.u > 0.f ? (double)c.u * mass : 0.0;
+        // the first in order whose sum passes the drawn one, else the last that stays
+        const bool hit = stays && upto > drawn;
+        const unsigned int first = wave_reduce(hit ? rank : 64u, MinOp{});
+        const unsigned int at = first < 64u ? first : wave_reduce(stays ? rank : 0u, MaxOp{});
+        if (rank == at) put_choice(p, row, (int)lane, (float)(-logit_depth(m, v, c.inv_t) - log(mass)));
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void top_wave_kernel(TopArgs p) {
+    const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
+    const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (unsigned long long row = blockIdx.x * 4ull + wave; row < p.x.rows; row += gridDim.x * 4ull) {
+        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
+        const unsigned int rank = __popcll(lanes_before(order_key(v), n));
+        const unsigned int allowed = __popcll(__ballot(v > -INFINITY));
+        if (rank < p.k && lane < n) {
+            const unsigned long long at = row * p.k + rank;
+            store_value(reinterpret_cast<T*>(p.values) + at, v);
+            p.index[at] = rank < allowed ? (int)lane : -1;
+        }
+        if (p.lse) {
+            const float m = wave_reduce(v, MaxOp{});
+            const double w = m > -INFINITY && m < INFINITY ? (double)__builtin_amdgcn_exp2f((v - m) * p.c2) : 0.0;
+            const double total = wave_reduce(w, SumOp{});
+            if (lane == 0) p.lse[row] = m == INFINITY || m == -INFINITY ? m : (float)((double)m * p.inv_t + log(total));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+// Workgroups of a launch: a row each, more rows than 2^18 in turn.
 unsigned int row_blocks(unsigned long long rows) { return (unsigned int)(rows < (1ull << 18) ? rows : (1ull << 18)); }
+
+// A row goes to the smallest workgroup whose registers hold it; longer ones are read again for every pass.
+template <typename T>
+hipError_t launch_choose(const ChooseArgs& a, hipStream_t st) {
+    const unsigned int n = a.x.n, blocks = row_blocks(a.x.rows);
+    if (n <= 64u) choose_wave_kernel<T><<<row_blocks((a.x.rows + 3) / 4), 256, 0, st>>>(a);
+    else if (n <= HeldRow<4, 2, T>::kMost) choose_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
+    else if (n <= HeldRow<8, 8, T>::kMost) choose_kernel<8, 8, T><<<blocks, 512, 0, st>>>(a);
+    else if (n <= HeldRow<16, 16, T>::kMost) choose_kernel<16, 16, T><<<blocks, 1024, 0, st>>>(a);
+    else choose_kernel<16, 0, T><<<blocks, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_top(const TopArgs& a, hipStream_t st) {
+    const unsigned int n = a.x.n, blocks = row_blocks(a.x.rows);
+    if (n <= 64u) top_wave_kernel<T><<<row_blocks((a.x.rows + 3) / 4), 256, 0, st>>>(a);
+    else if (n <= HeldRow<4, 2, T>::kMost) top_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
+    else if (n <= HeldRow<8, 8, T>::kMost) top_kernel<8, 8, T><<<blocks, 512, 0, st>>>(a);
+    else if (n <= HeldRow<16, 16, T>::kMost) top_kernel<16, 16, T><<<blocks, 1024, 0, st>>>(a);
+    else top_kernel<16, 0, T><<<blocks, 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
 
 }  // namespace
 }  // namespace rp
@@ -324,12 +948,7 @@ rp_status rp_choose_actions(const rp_rows* logits, const rp_choice* how, const f
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const rp::ChooseArgs a{rp::logit_rows(logits), how->temperature, how->top_p, how->min_p, how->top_k,
                            how->row_temperature, how->row_top_p, how->row_min_p, how->row_top_k, u, index, logp};
-    const dim3 grid(rp::row_blocks(logits->rows));
-    if (logits->dtype == RP_BF16)
-        hipLaunchKernelGGL((rp::choose_search_kernel<4, unsigned short>), grid, dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((rp::choose_search_kernel<4, float>), grid, dim3(256), 0, st, a);
-    RP_CHECK_HIP(hipGetLastError());
+    RP_CHECK_HIP(logits->dtype == RP_BF16 ? rp::launch_choose<unsigned short>(a, st) : rp::launch_choose<float>(a, st));
     return RP_OK;
 }
 
@@ -356,13 +975,9 @@ rp_status rp_top_actions(const rp_rows* logits, uint32_t k, double temperature, 
     (void)workspace;
     (void)bytes;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const rp::TopArgs a{rp::logit_rows(logits), k, 1.0 / temperature, static_cast<unsigned char*>(values), index, lse};
-    const dim3 grid(rp::row_blocks(logits->rows));
-    if (logits->dtype == RP_BF16)
-        hipLaunchKernelGGL((rp::top_search_kernel<4, unsigned short>), grid, dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((rp::top_search_kernel<4, float>), grid, dim3(256), 0, st, a);
-    RP_CHECK_HIP(hipGetLastError());
+    const rp::TopArgs a{rp::logit_rows(logits), k, 1.0 / temperature, (float)(1.4426950408889634 / temperature),
+                        static_cast<unsigned char*>(values), index, lse};
+    RP_CHECK_HIP(logits->dtype == RP_BF16 ? rp::launch_top<unsigned short>(a, st) : rp::launch_top<float>(a, st));
     return RP_OK;
 }
 

@@ -24,6 +24,89 @@ __device__ __forceinline__ float logit_value(const unsigned short* p) { return _
 // equal keys.
 __device__ __forceinline__ float clean_logit(float x) { return fmaxf(x, -INFINITY) + 0.f; }
 
+// 16 bytes of a row, at any alignment the row's elements have.
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+template <typename T>
+constexpr unsigned int kPerLoad = 16 / sizeof(T);
+template <typename T>
+__device__ __forceinline__ float element(const u32x4& raw, int e) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[e]);
+    else return __uint_as_float(e & 1 ? raw[e >> 1] & 0xFFFF0000u : raw[e >> 1] << 16);
+}
+// A thread's elements i .. of a row that ends at `end` (and has a load's worth of elements at least): the load
+// that would pass the end is moved back to it, and what belongs to the thread before comes as -infinity.
+template <typename T>
+__device__ __forceinline__ unsigned int load_place(unsigned int i, unsigned int end) { return min(i, end - kPerLoad<T>); }
+template <typename T>
+__device__ __forceinline__ void mask_moved(u32x4& raw, unsigned int i, unsigned int place) {
+    if (place == i) return;
+    const unsigned int gone = i - place;   // elements of the load that are not this thread's
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) {
+            if ((unsigned int)j < gone) raw[j] = 0xFF800000u;
+        } else {
+            if (2u * j < gone) raw[j] = (raw[j] & 0xFFFF0000u) | 0xFF80u;
+            if (2u * j + 1u < gone) raw[j] = (raw[j] & 0xFFFFu) | 0xFF800000u;
+        }
+    }
+}
+
+// A row, or a piece of one, spread over a workgroup's registers: NV loads of 16 bytes a thread.  `each` hands
+// every element to f(value, place in the row); what is past the end comes as -infinity.
+template <int W, int NV, typename T>
+struct HeldRow {
+    u32x4 raw[NV];
+    unsigned int first, last;   // the thread's first element; where the row's last load starts
+    static constexpr unsigned int kStep = 64u * W * kPerLoad<T>;
+    static constexpr unsigned int kMost = NV * kStep;
+    __device__ __forceinline__ HeldRow(const T* x, unsigned int begin, unsigned int end) {
+        first = begin + threadIdx.x * kPerLoad<T>;
+        last = end - kPerLoad<T>;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            raw[v] = *reinterpret_cast<const u32x4_any*>(x + min(first + v * kStep, last));
+#pragma unroll
+        for (int v = 0; v < NV; ++v) mask_moved<T>(raw[v], first + v * kStep, min(first + v * kStep, last));
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            // (each pass decodes the elements, and works out their places, anew: kept from one pass to the next
+            // they would fill the registers)
+            u32x4 r = raw[v];
+            unsigned int at = first;
+            asm volatile("" : "+v"(r), "+v"(at));
+            at = min(at + v * kStep, last);
+#pragma unroll
+            for (int e = 0; e < (int)kPerLoad<T>; ++e) f(element<T>(r, e), at + e, e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
+// The same interface over memory, for rows that registers do not hold: every `each` reads the row again.
+template <int W, typename T>
+struct ReadRow {
+    const T* x;
+    unsigned int begin, end;
+    __device__ __forceinline__ ReadRow(const T* x_, unsigned int begin_, unsigned int end_) : x(x_), begin(begin_), end(end_) {}
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        constexpr unsigned int kStep = 64u * W * kPerLoad<T>;
+#pragma unroll 4
+        for (unsigned int i = begin + threadIdx.x * kPerLoad<T>; i < end; i += kStep) {
+            const unsigned int at = load_place<T>(i, end);
+            u32x4 raw = *reinterpret_cast<const u32x4_any*>(x + at);
+            mask_moved<T>(raw, i, at);
+#pragma unroll
+            for (int e = 0; e < (int)kPerLoad<T>; ++e) f(element<T>(raw, e), at + e, e);
+        }
+    }
+};
+
 // Unsigned integers in the order of the floats.
 __device__ __forceinline__ unsigned int order_key(float x) {
     const unsigned int b = __float_as_uint(x);
@@ -32,6 +115,7 @@ __device__ __forceinline__ unsigned int order_key(float x) {
 __device__ __forceinline__ float key_value(unsigned int k) {
     return __uint_as_float(k ^ ((unsigned int)((int)~k >> 31) | 0x80000000u));
 }
+__device__ __forceinline__ unsigned int logit_key(float x) { return order_key(clean_logit(x)); }
 constexpr unsigned int kMaskedKey = 0x007FFFFFu;   // order_key(-infinity)
 
 // An action in the order of choice as one number, the first the largest: falling logit, rising index.

@@ -44,7 +44,7 @@ struct SearchShared {
 
 // Sums over the row: the weights and the number of the logits that `in` takes.
 template <int W, typename T, typename In>
-__device__ void search_sum(const T* x, unsigned int n, float m, double inv_t, In in, SearchShared<W>& s, unsigned int& turn,
+__device__ void search_sum(const Global<T>* x, unsigned int n, float m, double inv_t, In in, SearchShared<W>& s, unsigned int& turn,
                            unsigned long long* mass, unsigned int* count) {
     unsigned long long a = 0;
     unsigned int c = 0;
@@ -63,7 +63,7 @@ __device__ void search_sum(const T* x, unsigned int n, float m, double inv_t, In
 
 // Place of the `c`-th (from 1) logit with key v, by index.
 template <int W, typename T>
-__device__ unsigned int search_equal(const T* x, unsigned int n, unsigned int v, unsigned int c, SearchShared<W>& s) {
+__device__ unsigned int search_equal(const Global<T>* x, unsigned int n, unsigned int v, unsigned int c, SearchShared<W>& s) {
     const unsigned int lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     unsigned int found = 0xFFFFFFFFu, before = 0;
 #pragma unroll 1
@@ -103,7 +103,7 @@ __device__ unsigned int search_key(unsigned int lo, unsigned int hi, Enough enou
 
 template <int W, typename T>
 __device__ void choose_by_search(const ChooseArgs& p, unsigned long long row, SearchShared<W>& s) {
-    const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
     const unsigned int n = p.x.n;
     unsigned int turn = 0;
     // the allowed logits' range and number
@@ -196,8 +196,8 @@ __device__ void choose_by_search(const ChooseArgs& p, unsigned long long row, Se
 }
 
 
-__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_value(unsigned short* p, float v) { *p = (unsigned short)(__float_as_uint(v) >> 16); }
+__device__ __forceinline__ void store_value(Global<float>* p, float v) { *p = v; }
+__device__ __forceinline__ void store_value(Global<unsigned short>* p, float v) { *p = (unsigned short)(__float_as_uint(v) >> 16); }
 
 // ------------------------------------------------------------------- one workgroup per row, by candidates
 constexpr unsigned int kBins = 2048;    // of the histogram of weights
@@ -710,7 +710,7 @@ template <int W, int NV, typename T>
 __global__ __launch_bounds__(64 * W) void choose_kernel(ChooseArgs p) {
     __shared__ ChooseShared<W> s;
     for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
-        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         __syncthreads();
         if constexpr (NV > 0) {
             const HeldRow<W, NV, T> held(x, 0, p.x.n);
@@ -727,14 +727,14 @@ template <int W, typename T>
 __device__ void put_top(const TopArgs& p, unsigned long long row, const unsigned long long* words, unsigned int count) {
     for (unsigned int j = threadIdx.x; j < p.k; j += 64 * W) {
         const unsigned long long at = row * p.k + j;
-        store_value(reinterpret_cast<T*>(p.values) + at, j < count ? key_value(word_key(words[j])) : -INFINITY);
+        store_value(global_out<T>(p.values) + at, j < count ? key_value(word_key(words[j])) : -INFINITY);
         p.index[at] = j < count ? (int)word_index(words[j]) : -1;
     }
 }
 
 // The first k actions by search: those above the k-th value in any order, then the first ones equal to it.
 template <int W, typename T>
-__device__ unsigned int top_by_search(const T* x, unsigned int n, unsigned int k, float m, ChooseShared<W>& s) {
+__device__ unsigned int top_by_search(const Global<T>* x, unsigned int n, unsigned int k, float m, ChooseShared<W>& s) {
     unsigned int turn = 0, allowed, above;
     search_sum<W>(x, n, m, 0.0, [](unsigned int) { return true; }, s.search, turn, nullptr, &allowed);
     k = min(k, allowed);
@@ -768,7 +768,7 @@ __device__ unsigned int top_by_search(const T* x, unsigned int n, unsigned int k
 }
 
 template <int W, int SLOTS, typename T, typename Row>
-__device__ void top_row(const Row& held, const TopArgs& p, unsigned long long row, const T* x, ChooseShared<W>& s) {
+__device__ void top_row(const Row& held, const TopArgs& p, unsigned long long row, const Global<T>* x, ChooseShared<W>& s) {
     const float m = row_max<W>(held, s);
     if (p.lse) {
         // (the sum of a load in 32 bits, sums of those in 64)
@@ -799,7 +799,7 @@ template <int W, int NV, typename T>
 __global__ __launch_bounds__(64 * W) void top_kernel(TopArgs p) {
     __shared__ ChooseShared<W> s;
     for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
-        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         __syncthreads();
         if constexpr (NV > 0) {
             const HeldRow<W, NV, T> held(x, 0, p.x.n);
@@ -834,7 +834,7 @@ __global__ __launch_bounds__(256) void choose_wave_kernel(ChooseArgs p) {
     const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
     const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (unsigned long long row = blockIdx.x * 4ull + wave; row < p.x.rows; row += gridDim.x * 4ull) {
-        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
         const RowChoice c = row_choice(p, row);
         const long long k = p.row_top_k ? (long long)p.row_top_k[row] : p.top_k;
@@ -877,13 +877,13 @@ __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs p) {
     const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
     const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (unsigned long long row = blockIdx.x * 4ull + wave; row < p.x.rows; row += gridDim.x * 4ull) {
-        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
+        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
         const unsigned int rank = __popcll(lanes_before(order_key(v), n));
         const unsigned int allowed = __popcll(__ballot(v > -INFINITY));
         if (rank < p.k && lane < n) {
             const unsigned long long at = row * p.k + rank;
-            store_value(reinterpret_cast<T*>(p.values) + at, v);
+            store_value(global_out<T>(p.values) + at, v);
             p.index[at] = rank < allowed ? (int)lane : -1;
         }
         if (p.lse) {

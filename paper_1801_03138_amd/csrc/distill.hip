@@ -18,201 +18,490 @@ struct DistillArgs {
     unsigned long long grad_stride;
 };
 
-__device__ __forceinline__ void store_gradient(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_gradient(unsigned short* p, float v) {
+__device__ __forceinline__ void store_gradient(Global<float>* p, float v) { *p = v; }
+__device__ __forceinline__ void store_gradient(Global<unsigned short>* p, float v) {
     *p = __builtin_bit_cast(unsigned short, (__bf16)v);
 }
 
 // exp((x - m) / temperature) for x <= m.  The difference comes first: it is small where the weight is large.
 __device__ __forceinline__ float weight_of(float x, float m, float c2) { return __builtin_amdgcn_exp2f((x - m) * c2); }
 
-// A running maximum and the sum of exp((x - max) / temperature) beside it.
+// exp of a number in 64 bits to 32 bits' precision and 64 bits' range: 2^whole times a 32-bit 2^rest.  For what ends in a
+// gradient of 32 bits; what the loss is made of is a small difference of large logarithms and takes exp().
+__device__ __forceinline__ double wide_exp(double d) {
+    const double t = (d < -1e4 ? -1e4 : d) * 1.4426950408889634, whole = rint(t);
+    return ldexp((double)__builtin_amdgcn_exp2f((float)(t - whole)), (int)whole);
+}
+
+// A maximum and the sum of exp((. - max) / temperature) beside it.
 struct MaxSum {
     float m;
     double s;
 };
-__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c2) {
-    const float m = fmaxf(a.m, b.m);
-    if (m == -INFINITY) return MaxSum{m, 0.0};
-    return MaxSum{m, (a.m == -INFINITY ? 0.0 : a.s * (double)weight_of(a.m, m, c2)) +
-                         (b.m == -INFINITY ? 0.0 : b.s * (double)weight_of(b.m, m, c2))};
-}
+
+// What a wavefront knows of the row's entries.
+struct EntryPart {
+    double tm, a, b, c;   // max of t / tt (REST: the teacher's log-sum-exp); sums of q' = exp(t / tt - tm), q' (t / tt - tm), q' z / ts
+    double z;             // sum of exp((z - zm) / ts), each action once
+    float zm;
+    unsigned int any;     // some entry is there with a logit above -infinity
+};
+
+// What every element's gradient needs, worked out once per row.
+struct RowScalars {
+    float m, factor;
+    double shift, q_scale, inside, scale, inv_total;
+    unsigned int state;   // 0: as computed; 1: nothing to learn, all 0; 2: all NaN
+};
 
 template <int W>
 struct DistillShared {
     MaxSum row[W];
-    float tmax[W], zmax[W];
-    double sums[W][4];
-    unsigned int twice;    // some action is in two entries
+    EntryPart part[W];
+    RowScalars out;
+    unsigned int twice;   // some action is in two entries
 };
 
-// One workgroup of W wavefronts per row.  LDS behind the arguments: which actions have an entry, a bit each
-// [(n + 31) / 32 words], and the entries' actions, teacher logits and student logits [k] each.
-template <int W, typename T, typename TT, bool REST, bool GRAD>
-__global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs p) {
-    extern __shared__ unsigned int lds[];
-    __shared__ DistillShared<W> s;
-    const unsigned int n = p.x.n, k = p.k, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    const unsigned int words = (n + 31u) / 32u;
-    unsigned int* named = lds;
-    int* act = reinterpret_cast<int*>(lds + words);
-    float* tv = reinterpret_cast<float*>(act + k);
-    float* zv = tv + k;
-    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
-        const T* x = reinterpret_cast<const T*>(p.x.data) + row * p.x.stride;
-        T* g = GRAD ? reinterpret_cast<T*>(p.grad) + row * p.grad_stride : nullptr;
-        const float weight = p.weight ? p.weight[row] : 1.f;
-        __syncthreads();   // (the row before is done with LDS)
-        if (weight == 0.f) {
-            if (tid == 0) p.loss[row] = 0.f;
-            if (GRAD)
-                for (unsigned int i = tid; i < n; i += 64 * W) store_gradient(g + i, 0.f);
-            continue;
-        }
-        // entries: mark their actions
-        for (unsigned int i = tid; i < words; i += 64 * W) named[i] = 0;
-        if (tid == 0) s.twice = 0;
-        __syncthreads();
-        float tmax = -INFINITY, zmax = -INFINITY;
-        bool bad = false;
-        for (unsigned int e = tid; e < k; e += 64 * W) {
-            const int a = p.entry[row * k + e];
-            const bool there = (unsigned int)a < n;
-            float t = there ? logit_value(reinterpret_cast<const TT*>(p.value) + row * k + e) : -INFINITY;
-            float z = there ? logit_value(x + a) : -INFINITY;
-            if (there) {
-                const unsigned int bit = 1u << (a & 31);
-                if (atomicOr(&named[a >> 5], bit) & bit) s.twice = 1;
-            }
-            act[e] = there ? a : -1;
-            tv[e] = t;
-            zv[e] = z;
-            bad |= !(t < INFINITY);
-            tmax = fmaxf(tmax, t);
-            zmax = fmaxf(zmax, z);
-        }
-        __syncthreads();
-        // the row: all of it, or (REST) what has no entry
-        MaxSum all{-INFINITY, 0.0};
-        for (unsigned int i = tid; i < n; i += 64 * W) {
-            const float v = logit_value(x + i);
-            bad |= !(v < INFINITY);
-            if (REST && (named[i >> 5] >> (i & 31u) & 1u)) continue;
-            if (v > all.m) {
-                all.s = all.m == -INFINITY ? 1.0 : all.s * (double)weight_of(all.m, v, p.c2) + 1.0;
-                all.m = v;
-            } else if (v > -INFINITY) {
-                all.s += (double)weight_of(v, all.m, p.c2);
-            }
-        }
-        const bool any_bad = __syncthreads_or(bad);
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            const MaxSum o{__shfl_xor(all.m, off, 64), __shfl_xor(all.s, off, 64)};
-            all = join(all, o, p.c2);
-            tmax = fmaxf(tmax, __shfl_xor(tmax, off, 64));
-            zmax = fmaxf(zmax, __shfl_xor(zmax, off, 64));
-        }
-        if (lane == 0) {
-            s.row[wave] = all;
-            s.tmax[wave] = tmax;
-            s.zmax[wave] = zmax;
-        }
-        __syncthreads();
-        all = s.row[0];
-        tmax = s.tmax[0];
-        zmax = s.zmax[0];
-        for (int w = 1; w < W; ++w) {
-            all = join(all, s.row[w], p.c2);
-            tmax = fmaxf(tmax, s.tmax[w]);
-            zmax = fmaxf(zmax, s.zmax[w]);
-        }
-        const float m = REST ? fmaxf(all.m, zmax) : all.m;
-        const bool empty = m == -INFINITY || (!REST && tmax == -INFINITY);
-        // sums over the entries: a_e = exp((t_e - shift) / tt), a_e (t_e - shift) / tt, a_e (z_e - m) / ts, and the
-        // student's weight of each action once
-        double sum[4] = {0.0, 0.0, 0.0, 0.0};
-        const double shift = REST ? (double)p.teacher_lse[row] : tmax == -INFINITY ? 0.0 : (double)tmax * p.inv_tt;
-        const bool twice = s.twice;
-        for (unsigned int e = tid; e < k; e += 64 * W) {
-            if (act[e] < 0) continue;
-            const double d = (double)tv[e] * p.inv_tt - shift;
-            const double a = exp(d), zd = ((double)zv[e] - (double)m) * p.inv_ts;
-            bool first = true;
-            if (twice)
-                for (unsigned int f = 0; f < e && first; ++f) first = act[f] != act[e];
-            sum[0] += a;
-            if (a > 0.0 || a != a) {
-                sum[1] += a * d;
-                sum[2] += a * zd;
-            }
-            if (first && !empty) sum[3] += exp(zd);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] = wave_reduce(sum[j], SumOp{});
-        if (lane == 0)
-            for (int j = 0; j < 4; ++j) s.sums[wave][j] = sum[j];
-        __syncthreads();
-        for (int j = 0; j < 4; ++j) {
-            sum[j] = s.sums[0][j];
-            for (int w = 1; w < W; ++w) sum[j] += s.sums[w][j];
-        }
-        // row scalars, the same in every thread.  total = sum of exp((x - m) / ts) over the row.
-        const double outer = all.m == -INFINITY ? 0.0 : all.s * exp(((double)all.m - (double)m) * p.inv_ts);
-        const double total = REST ? outer + sum[3] : outer;
-        const double log_total = log(total);
-        double loss, q_scale, inside, outside;
-        if (!REST) {
-            q_scale = 1.0 / sum[0];
-            loss = (sum[1] - sum[2]) * q_scale - log(sum[0]) + log_total;
-            inside = outside = 1.0;
-        } else {
-            const double sum_q = sum[0], sum_p = sum[3] / total, p_rest = outer / total;
-            q_scale = 1.0;
-            loss = sum[1] - sum[2] + sum_q * log_total;
-            inside = outside = sum_q;
-            if (sum_q < 1.0 && p_rest > 0.0) {
-                loss += (1.0 - sum_q) * (log1p(-sum_q) - (sum_p < 0.5 ? log1p(-sum_p) : log(p_rest)));
-                inside = 1.0;
-                outside = (sum_q - sum_p) / p_rest;
-            }
-        }
-        if (any_bad) loss = NAN;
-        if (tid == 0) p.loss[row] = empty && !any_bad ? 0.f : (float)(loss * (double)weight);
-        if (!GRAD) continue;
-        const double scale = (double)weight * p.inv_ts;
-        const float factor = any_bad ? NAN : empty ? 0.f : (float)(scale * outside / total);
-        for (unsigned int i = tid; i < n; i += 64 * W)
-            store_gradient(g + i, empty && !any_bad ? 0.f : factor * weight_of(logit_value(x + i), m, p.c2));
-        __syncthreads();   // (an action with an entry is written again below)
-        if (empty || any_bad) continue;
-        for (unsigned int e = tid; e < k; e += 64 * W) {
-            if (act[e] < 0) continue;
-            double q = exp((double)tv[e] * p.inv_tt - shift) * q_scale;
-            if (twice) {   // the first of an action's entries writes, with the sum of all
-                bool first = true;
-                q = 0.0;
-                for (unsigned int f = 0; f < k; ++f)
-                    if (act[f] == act[e]) {
-                        first &= f >= e;
-                        q += exp((double)tv[f] * p.inv_tt - shift) * q_scale;
-                    }
-                if (!first) continue;
-            }
-            const double pe = exp(((double)zv[e] - (double)m) * p.inv_ts) / total;
-            store_gradient(g + act[e], (float)(scale * (pe * inside - q)));
+// The entries of a row in LDS, in arrays of k.
+struct Entries {
+    int* act;       // -1: no entry
+    float *t, *z;   // the teacher's and the student's logit
+};
+
+// Puts the row's entries into LDS and marks the actions among `begin` .. `end` that have one, a bit each, in `named`
+// (cleared before, one word more than the range needs).
+template <int W, typename T, typename TT, bool MARK>
+__device__ __forceinline__ void load_entries(const DistillArgs& p, unsigned long long row, const Global<T>* x, const float* z_given,
+                                             unsigned int begin, unsigned int end, Entries en, unsigned int* named,
+                                             DistillShared<W>& s) {
+    const unsigned int k = p.k;
+#pragma unroll 1
+    for (unsigned int e = threadIdx.x; e < k; e += 64 * W) {
+        const int a = global_in<int>(p.entry)[row * k + e];
+        const bool there = (unsigned int)a < p.x.n;
+        en.act[e] = there ? a : -1;
+        en.t[e] = there ? logit_value(global_in<TT>(p.value) + row * k + e) : -INFINITY;
+        en.z[e] = !there ? -INFINITY : z_given ? global_in<float>(z_given)[row * k + e] : logit_value(x + a);
+        if (MARK && there && (unsigned int)a >= begin && (unsigned int)a < end) {
+            const unsigned int at = a - begin, bit = 1u << (at & 31u);
+            if (atomicOr(&named[at >> 5], bit) & bit) s.twice = 1;
         }
     }
 }
 
-template <typename T, typename TT, bool GRAD>
-void launch_distill(const DistillArgs& a, hipStream_t st) {
-    const unsigned int blocks = (unsigned int)(a.x.rows < (1ull << 18) ? a.x.rows : (1ull << 18));
-    const size_t lds = ((a.x.n + 31u) / 32u + 3u * a.k) * 4u;
-    if (a.teacher_lse)
-        hipLaunchKernelGGL((distill_kernel<4, T, TT, true, GRAD>), dim3(blocks), dim3(256), lds, st, a);
-    else
-        hipLaunchKernelGGL((distill_kernel<4, T, TT, false, GRAD>), dim3(blocks), dim3(256), lds, st, a);
+// Sums over the wavefront's share of the entries.
+template <int W, bool REST>
+__device__ __forceinline__ void sum_entries(const DistillArgs& p, unsigned long long row, Entries en, DistillShared<W>& s) {
+    const unsigned int tid = threadIdx.x, wave = tid >> 6, k = p.k;
+    EntryPart r{-INFINITY, 0.0, 0.0, 0.0, 0.0, -INFINITY, 0};
+    if (__builtin_amdgcn_readfirstlane(wave * 64u) < k) {
+        float tm = -INFINITY;
+        bool bad = false;
+#pragma unroll 1
+        for (unsigned int e = tid; e < k; e += 64 * W) {
+            tm = fmaxf(tm, en.t[e]);
+            r.zm = fmaxf(r.zm, en.z[e]);
+            bad |= en.act[e] >= 0 && !(en.t[e] < INFINITY);
+        }
+        tm = wave_reduce(tm, MaxOp{});
+        r.zm = wave_reduce(r.zm, MaxOp{});
+        r.any = tm > -INFINITY;
+        r.tm = REST ? (double)global_in<float>(p.teacher_lse)[row] : (double)tm * p.inv_tt;
+        const double tm0 = REST || r.any ? r.tm : 0.0, zm0 = r.zm > -INFINITY ? (double)r.zm : 0.0;
+        const bool twice = s.twice;
+#pragma unroll 1
+        for (unsigned int e = tid; e < k; e += 64 * W) {
+            if (en.act[e] < 0) continue;
+            const double d = (double)en.t[e] * p.inv_tt - tm0, z = (double)en.z[e];
+            bool first = true;
+            if (twice)
+#pragma unroll 1
+                for (unsigned int f = 0; f < e && first; ++f) first = en.act[f] != en.act[e];
+            // (one exp after the other: side by side they would take the registers that hold the row)
+#pragma unroll 1
+            for (int which = 0; which < 2; ++which) {
+                const double v = exp(which ? (z - zm0) * p.inv_ts : d);
+                if (which) {
+                    if (first) r.z += v;
+                } else {
+                    r.a += v;
+                    if (!(v == 0.0)) {
+                        r.b += v * d;
+                        r.c += v * z * p.inv_ts;
+                    }
+                }
+            }
+        }
+        if (bad) r.a = NAN;
+        r.a = wave_reduce(r.a, SumOp{});
+        r.b = wave_reduce(r.b, SumOp{});
+        r.c = wave_reduce(r.c, SumOp{});
+        r.z = wave_reduce(r.z, SumOp{});
+    }
+    if ((tid & 63u) == 0) s.part[wave] = r;
+}
+
+// Maximum and sum over what `row` holds, of what has no entry (REST) or all of it, the same in the lanes of a wavefront.
+// `named` has a bit for every action from `begin` on; `again`: the same elements, read from memory.
+template <bool REST, typename T, typename Row, typename Again>
+__device__ __forceinline__ MaxSum sum_row(const Row& row, const Again& again, unsigned int begin, const unsigned int* named,
+                                          float c2) {
+    constexpr int kN = (int)kPerLoad<T>;
+    constexpr unsigned int kAll = (1u << kN) - 1u;
+    // which elements of a load do not count here
+    auto bits_out = [&](unsigned int i, unsigned int gone) -> unsigned int {
+        unsigned int bits = (1u << min(gone, (unsigned int)kN)) - 1u;
+        if (REST) {
+            const unsigned int at = i - begin;
+            const unsigned long long two = (unsigned long long)named[(at >> 5) + 1u] << 32 | named[at >> 5];
+            bits |= (unsigned int)(two >> (at & 31u)) & kAll;
+        }
+        return bits;
+    };
+    if constexpr (!Row::kHeld) {
+        // one pass: a thread's own running maximum, to which its sum is brought when it rises
+        float m = -INFINITY;
+        double sum = 0.0;
+        row.each_load([&](u32x4 raw, unsigned int i, unsigned int gone) {
+            const unsigned int bits = bits_out(i, gone);
+            float top = -INFINITY, load = 0.f;
+            if (bits) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) top = fmaxf(top, bits >> e & 1u ? -INFINITY : element<T>(raw, e));
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) top = fmaxf(top, element<T>(raw, e));
+            }
+            if (top > m) {
+                sum *= (double)weight_of(m, top, c2);
+                m = top;
+            }
+            const float m0 = m > -INFINITY ? m : 0.f;
+            if (bits) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) load += bits >> e & 1u ? 0.f : weight_of(element<T>(raw, e), m0, c2);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) load += weight_of(element<T>(raw, e), m0, c2);
+            }
+            sum += (double)load;
+        });
+        const float all = wave_reduce(m, MaxOp{});
+        const double back = sum == 0.0 ? 0.0 : sum * (double)(m > -INFINITY ? weight_of(m, all, c2) : 1.f);
+        return MaxSum{all, wave_reduce(back, SumOp{})};
+    } else {
+    // (the sum of a load in 32 bits, sums of those in 64)
+    auto sum_to = [&](const auto& r, float m0) {
+        double sum = 0.0;
+        r.each_load([&](u32x4 raw, unsigned int i, unsigned int gone) {
+            const unsigned int bits = bits_out(i, gone);
+            float load = 0.f;
+            if (bits) {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) load += bits >> e & 1u ? 0.f : weight_of(element<T>(raw, e), m0, c2);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kN; ++e) load += weight_of(element<T>(raw, e), m0, c2);
+            }
+            sum += (double)load;
+        });
+        return wave_reduce(sum, SumOp{});
+    };
+    float m = -INFINITY;
+    row.each_load([&](u32x4 raw, unsigned int, unsigned int) {
+#pragma unroll
+        for (int e = 0; e < kN; ++e) m = fmaxf(m, element<T>(raw, e));
+    });
+    m = wave_reduce(m, MaxOp{});
+    double sum = sum_to(row, m > -INFINITY ? m : 0.f);
+    if (REST && sum < 1e-20) {
+        // what has no entry lies so far below what has one that 32 bits lose it: once more, from its own maximum
+        m = -INFINITY;
+        again.each_load([&](u32x4 raw, unsigned int i, unsigned int gone) {
+            const unsigned int bits = bits_out(i, gone);
+#pragma unroll
+            for (int e = 0; e < kN; ++e) m = fmaxf(m, bits >> e & 1u ? -INFINITY : element<T>(raw, e));
+        });
+        m = wave_reduce(m, MaxOp{});
+        sum = sum_to(again, m > -INFINITY ? m : 0.f);
+    }
+    return MaxSum{m, sum};
+    }
+}
+
+// Sum over the lanes of each quarter of a wavefront, in all of them.
+__device__ __forceinline__ double quarter_sum(double v) {
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
+// From the parts of the row and of its entries to the loss and what the gradient needs.  Called by one wavefront.  There
+// are up to 16 parts of either kind: its quarters bring the sums over the row, over the entries' student weights and over
+// the teacher's to one maximum, with one exp for all, and one log serves for the logarithms too.
+template <bool REST>
+__device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long long row, float weight, const EntryPart* part,
+                                           unsigned int parts, const MaxSum* rows, unsigned int pieces, RowScalars* out) {
+    const unsigned int lane = threadIdx.x & 63u, quarter = lane >> 4, l = lane & 15u;
+    const bool part_here = l < parts, row_here = l < pieces;
+    const EntryPart& r = part[part_here ? l : 0u];
+    const MaxSum& x = rows[row_here ? l : 0u];
+    const float own_z = part_here ? r.zm : -INFINITY, own_x = row_here ? x.m : -INFINITY;
+    const bool own_any = part_here && r.any;
+    const double own_t = own_any ? r.tm : -INFINITY;
+    const float zm = wave_reduce(own_z, MaxOp{}), xm = wave_reduce(own_x, MaxOp{});
+    const bool any = __ballot(own_any) != 0;
+    const float m = REST ? fmaxf(zm, xm) : xm;
+    const double m0 = m > -INFINITY ? (double)m : 0.0;
+    const double tm = wave_reduce(own_t, MaxOp{});
+    const double shift = REST ? (double)global_in<float>(p.teacher_lse)[row] : any ? tm : 0.0;
+    double from = quarter == 0 ? (own_x > -INFINITY ? ((double)own_x - m0) * p.inv_ts : 0.0)
+                  : quarter == 1 ? (own_z > -INFINITY ? ((double)own_z - m0) * p.inv_ts : 0.0)
+                                 : (!REST && own_any ? own_t - shift : 0.0);
+    const double factor = exp(from);
+    double first = quarter == 0 ? (row_here ? x.s : 0.0) : quarter == 1 ? (part_here ? r.z : 0.0) : (part_here ? r.a : 0.0);
+    double b = part_here ? r.b : 0.0, c = part_here ? r.c : 0.0;
+    // (q' (t - tm) from a wavefront's own maximum to the row's)
+    if (!REST && quarter >= 2u) b = first == 0.0 ? 0.0 : (b + first * from) * factor;
+    if (!REST) c = factor == 0.0 ? 0.0 : c * factor;
+    first = quarter_sum(first == 0.0 ? 0.0 : first * factor);
+    b = __shfl(quarter_sum(b), 32, 64);
+    c = __shfl(quarter_sum(c), 32, 64);
+    const double outer = __shfl(first, 0, 64), inner = __shfl(first, 16, 64), a = __shfl(first, 32, 64);
+    const double total = REST ? outer + inner : outer, p_in = inner / total, p_rest = outer / total;
+    // (in 64 bits log(1 - v) is as good as log1p(-v) for what is multiplied by 1 - v and added to the rest)
+    const double logs = log(lane == 0   ? total
+                            : lane == 1 ? (REST ? 1.0 - a : a)
+                                        : (p_in < 0.5 ? 1.0 - p_in : p_rest));
+    const double log_total = __shfl(logs, 0, 64) + m0 * p.inv_ts, log_a = __shfl(logs, 1, 64), log_rest = __shfl(logs, 2, 64);
+    double loss, q_scale = 1.0, inside = 1.0, outside = 1.0;
+    if (!REST) {
+        q_scale = 1.0 / a;
+        loss = (b - c) * q_scale - log_a + log_total;
+    } else {
+        loss = b - c + a * log_total;
+        inside = outside = a;
+        if (a < 1.0 && p_rest > 0.0) {
+            loss += (1.0 - a) * (log_a - log_rest);
+            inside = 1.0;
+            outside = (a - p_in) / p_rest;
+        }
+    }
+    // (NaN and +infinity anywhere have made one of the sums NaN)
+    const bool bad = !(total < INFINITY) || a != a;
+    const bool empty = !bad && (m == -INFINITY || (!REST && !any));
+    if (bad) loss = NAN;
+    if (lane == 0) {
+        p.loss[row] = empty ? 0.f : (float)(loss * (double)weight);
+        const double scale = (double)weight * p.inv_ts;
+        *out = RowScalars{m > -INFINITY ? m : 0.f, bad ? NAN : (float)(scale * outside / total), shift, q_scale, inside, scale,
+                          1.0 / total, empty ? 1u : bad ? 2u : 0u};
+    }
+}
+
+__device__ __forceinline__ unsigned int bf16_pair_of(float lo, float hi) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned int, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+
+// The gradient of what `row` holds as if nothing of it had an entry.  Where two threads' loads share elements, at the row's
+// end, both store the same values if the row is held; else, as the gradient may lie over the logits, each element is read
+// by the thread that stores it alone.
+template <typename T, typename Row>
+__device__ __forceinline__ void put_gradient(const Row& row, Global<T>* g, const RowScalars& o, float c2) {
+    const float m = o.m, factor = o.state == 1u ? 0.f : o.factor;
+    row.each_load([&](u32x4 raw, unsigned int i, unsigned int gone) {
+        if constexpr (!Row::kHeld) {
+            if (gone) {
+                for (unsigned int e = gone; e < kPerLoad<T>; ++e)
+                    store_gradient(g + i + e, factor * weight_of(logit_value(row.x + i + e), m, c2));
+                return;
+            }
+        }
+        auto value = [&](int e) { return factor * weight_of(element<T>(raw, e), m, c2); };
+        u32x4 out;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 4) out[j] = __float_as_uint(value(j));
+            else out[j] = bf16_pair_of(value(2 * j), value(2 * j + 1));
+        }
+        *(Global<u32x4_any>*)(g + i) = out;
+    });
+}
+
+// The gradient of the actions among begin .. end that have an entry.
+template <int W, typename T>
+__device__ __forceinline__ void put_entries(const DistillArgs& p, Global<T>* g, Entries en, unsigned int begin, unsigned int end,
+                                            const RowScalars& o, bool twice) {
+    const unsigned int k = p.k;
+#pragma unroll 1
+    for (unsigned int e = threadIdx.x; e < k; e += 64 * W) {
+        const unsigned int a = (unsigned int)en.act[e];
+        if (a < begin || a >= end) continue;   // (-1 is beyond any end)
+        double q = wide_exp((double)en.t[e] * p.inv_tt - o.shift) * o.q_scale;
+        if (twice) {   // the first of an action's entries writes, with the sum of all
+            bool first = true;
+            q = 0.0;
+#pragma unroll 1
+            for (unsigned int f = 0; f < k; ++f)
+                if (en.act[f] == (int)a) {
+                    first &= f >= e;
+                    q += wide_exp((double)en.t[f] * p.inv_tt - o.shift) * o.q_scale;
+                }
+            if (!first) continue;
+        }
+        const double pe = wide_exp(((double)en.z[e] - (double)o.m) * p.inv_ts) * o.inv_total;
+        store_gradient(g + a, (float)(o.scale * (pe * o.inside - q)));
+    }
+}
+
+template <int W, typename T>
+__device__ __forceinline__ void put_zeros(Global<T>* g, unsigned int n) {
+    for (unsigned int i = threadIdx.x; i < n; i += 64 * W) store_gradient(g + i, 0.f);
+}
+
+// A row of up to 64 NV elements in the registers of one wavefront, element by element: no load is too long for it.
+template <int NV, typename T>
+struct ShortRow {
+    float v[NV];
+    __device__ __forceinline__ ShortRow(const Global<T>* x, unsigned int n) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const unsigned int i = threadIdx.x + 64u * j;
+            v[j] = i < n ? logit_value(x + i) : -INFINITY;
+        }
+    }
+};
+
+// Rows of up to 64 NV actions: one wavefront each.
+template <int NV, typename T, typename TT, bool REST, bool GRAD>
+__global__ __launch_bounds__(64) void distill_wave_kernel(DistillArgs p) {
+    extern __shared__ unsigned int lds[];
+    __shared__ DistillShared<1> s;
+    const unsigned int n = p.x.n, k = p.k, lane = threadIdx.x;
+    constexpr unsigned int kWords = 2u * NV;
+    unsigned int* named = lds;
+    const Entries en{reinterpret_cast<int*>(lds + kWords), reinterpret_cast<float*>(lds + kWords + k),
+                     reinterpret_cast<float*>(lds + kWords + 2u * k)};
+    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
+        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+        Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
+        const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
+        __syncthreads();
+        if (weight == 0.f) {
+            if (lane == 0) p.loss[row] = 0.f;
+            if (GRAD) put_zeros<1, T>(g, n);
+            continue;
+        }
+        const ShortRow<NV, T> held(x, n);
+        if (lane < kWords) named[lane] = 0;
+        if (lane == 0) s.twice = 0;
+        __syncthreads();
+        load_entries<1, T, TT, true>(p, row, x, nullptr, 0, n, en, named, s);
+        __syncthreads();
+        sum_entries<1, REST>(p, row, en, s);
+        float m = -INFINITY;
+        bool out[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const unsigned int i = lane + 64u * j;
+            out[j] = REST && (named[i >> 5] >> (i & 31u) & 1u);
+            m = fmaxf(m, out[j] ? -INFINITY : held.v[j]);
+        }
+        m = wave_reduce(m, MaxOp{});
+        const float m0 = m > -INFINITY ? m : 0.f;
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) sum += out[j] ? 0.0 : (double)weight_of(held.v[j], m0, p.c2);
+        sum = wave_reduce(sum, SumOp{});
+        if (lane == 0) s.row[0] = MaxSum{m, sum};
+        __syncthreads();
+        finish_row<REST>(p, row, weight, s.part, 1, s.row, 1, &s.out);
+        if (!GRAD) continue;
+        __syncthreads();
+        const RowScalars o = s.out;
+        const float factor = o.state == 1u ? 0.f : o.factor;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const unsigned int i = lane + 64u * j;
+            if (i < n) store_gradient(g + i, factor * weight_of(held.v[j], o.m, p.c2));
+        }
+        __syncthreads();   // (an action with an entry is written again)
+        if (o.state == 0) put_entries<1, T>(p, g, en, 0, n, o, s.twice != 0);
+    }
+}
+
+template <int W, typename T, typename TT, bool REST, bool GRAD, typename Row>
+__device__ __forceinline__ void distill_row(const DistillArgs& p, unsigned long long row, float weight, const Global<T>* x,
+                                            Global<T>* g, const Row& held, unsigned int* named, unsigned int words,
+                                            Entries en, DistillShared<W>& s) {
+    const unsigned int tid = threadIdx.x, n = p.x.n;
+    for (unsigned int i = tid; i < words; i += 64 * W) named[i] = 0;
+    if (tid == 0) s.twice = 0;
+    __syncthreads();
+    load_entries<W, T, TT, REST || GRAD>(p, row, x, nullptr, 0, n, en, named, s);
+    __syncthreads();
+    sum_entries<W, REST>(p, row, en, s);
+    const MaxSum mine = sum_row<REST, T>(held, ReadRow<W, T, 1>(x, 0, n), 0, named, p.c2);
+    if ((tid & 63u) == 0) s.row[tid >> 6] = mine;
+    __syncthreads();
+    if (tid < 64) finish_row<REST>(p, row, weight, s.part, W, s.row, W, &s.out);
+    if (!GRAD) return;
+    __syncthreads();
+    put_gradient<T>(held, g, s.out, p.c2);
+    __syncthreads();   // (an action with an entry is written again)
+    if (s.out.state == 0) put_entries<W, T>(p, g, en, 0, n, s.out, s.twice != 0);
+}
+
+// One workgroup of W wavefronts per row, held in registers (NV > 0) or read again for each of three passes.  LDS
+// behind the arguments: the marks, (n + 31) / 32 + 1 words, and the entries.
+template <int W, int NV, int EU, typename T, typename TT, bool REST, bool GRAD>
+__global__ __launch_bounds__(64 * W, EU) void distill_kernel(DistillArgs p) {
+    extern __shared__ unsigned int lds[];
+    __shared__ DistillShared<W> s;
+    const unsigned int n = p.x.n, k = p.k;
+    const unsigned int words = (n + 31u) / 32u + 1u;
+    const Entries en{reinterpret_cast<int*>(lds + words), reinterpret_cast<float*>(lds + words + k),
+                     reinterpret_cast<float*>(lds + words + 2u * k)};
+    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
+        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+        Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
+        const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
+        __syncthreads();   // (the row before is done with LDS)
+        if (weight == 0.f) {
+            if (threadIdx.x == 0) p.loss[row] = 0.f;
+            if (GRAD) put_zeros<W, T>(g, n);
+        } else if constexpr (NV > 0) {
+            distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, HeldRow<W, NV, T, false>(x, 0, n), lds, words, en, s);
+        } else {
+            distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, ReadRow<W, T>(x, 0, n), lds, words, en, s);
+        }
+    }
+}
+
+template <typename T, typename TT, bool REST, bool GRAD>
+hipError_t launch_rows(const DistillArgs& a, hipStream_t st) {
+    const unsigned int n = a.x.n, blocks = (unsigned int)(a.x.rows < (1ull << 18) ? a.x.rows : (1ull << 18));
+    const size_t lds = ((n + 31u) / 32u + 1u + 3u * a.k) * 4u;
+    if (n <= 256u) {
+        distill_wave_kernel<4, T, TT, REST, GRAD><<<blocks, 64, (8u + 3u * a.k) * 4u, st>>>(a);
+    } else if constexpr (!GRAD) {
+        if (n <= 2048u) distill_kernel<1, 0, 4, T, TT, REST, GRAD><<<blocks, 64, lds, st>>>(a);
+        else distill_kernel<4, 0, 4, T, TT, REST, GRAD><<<blocks, 256, lds, st>>>(a);
+    } else {
+        if (n <= HeldRow<1, 4, T>::kMost) distill_kernel<1, 4, 4, T, TT, REST, GRAD><<<blocks, 64, lds, st>>>(a);
+        else if (n <= HeldRow<2, 8, T>::kMost) distill_kernel<2, 8, 3, T, TT, REST, GRAD><<<blocks, 128, lds, st>>>(a);
+        else if (n <= HeldRow<4, 8, T>::kMost) distill_kernel<4, 8, 4, T, TT, REST, GRAD><<<blocks, 256, lds, st>>>(a);
+        else if (n <= HeldRow<4, 16, T>::kMost) distill_kernel<4, 16, 3, T, TT, REST, GRAD><<<blocks, 256, lds, st>>>(a);
+        else distill_kernel<8, 0, 4, T, TT, REST, GRAD><<<blocks, 512, lds, st>>>(a);
+    }
+    return hipGetLastError();
+}
+template <typename T, typename TT>
+hipError_t launch_distill(const DistillArgs& a, bool gradient, hipStream_t st) {
+    if (a.teacher_lse) return gradient ? launch_rows<T, TT, true, true>(a, st) : launch_rows<T, TT, true, false>(a, st);
+    return gradient ? launch_rows<T, TT, false, true>(a, st) : launch_rows<T, TT, false, false>(a, st);
 }
 
 rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad,
@@ -247,13 +536,8 @@ rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* tea
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const bool xb = logits->dtype == RP_BF16, tb = teacher->dtype == RP_BF16;
     typedef unsigned short B;
-    if (gradient)
-        xb ? (tb ? launch_distill<B, B, true>(a, st) : launch_distill<B, float, true>(a, st))
-           : (tb ? launch_distill<float, B, true>(a, st) : launch_distill<float, float, true>(a, st));
-    else
-        xb ? (tb ? launch_distill<B, B, false>(a, st) : launch_distill<B, float, false>(a, st))
-           : (tb ? launch_distill<float, B, false>(a, st) : launch_distill<float, float, false>(a, st));
-    RP_CHECK_HIP(hipGetLastError());
+    RP_CHECK_HIP(xb ? (tb ? launch_distill<B, B>(a, gradient, st) : launch_distill<B, float>(a, gradient, st))
+                    : (tb ? launch_distill<float, B>(a, gradient, st) : launch_distill<float, float>(a, gradient, st)));
     return RP_OK;
 }
 

@@ -17,8 +17,17 @@ struct LogitRows {
     unsigned int n;
 };
 
-__device__ __forceinline__ float logit_value(const float* p) { return *p; }
-__device__ __forceinline__ float logit_value(const unsigned short* p) { return __uint_as_float((unsigned int)*p << 16); }
+// Pointers to global memory by their type: a pointer whose memory the compiler has to find out at run time costs a load
+// that also counts as one of LDS.
+template <typename T>
+using Global = T __attribute__((address_space(1)));
+template <typename T>
+__device__ __forceinline__ const Global<T>* global_in(const void* p) { return (const Global<T>*)p; }
+template <typename T>
+__device__ __forceinline__ Global<T>* global_out(void* p) { return (Global<T>*)p; }
+
+__device__ __forceinline__ float logit_value(const Global<float>* p) { return *p; }
+__device__ __forceinline__ float logit_value(const Global<unsigned short>* p) { return __uint_as_float((unsigned int)*p << 16); }
 
 // What is not allowed (NaN, -infinity) becomes -infinity and -0 becomes +0, so that equal logits have
 // equal keys.
@@ -54,21 +63,40 @@ __device__ __forceinline__ void mask_moved(u32x4& raw, unsigned int i, unsigned 
 }
 
 // A row, or a piece of one, spread over a workgroup's registers: NV loads of 16 bytes a thread.  `each` hands
-// every element to f(value, place in the row); what is past the end comes as -infinity.
-template <int W, int NV, typename T>
+// every element to f(value, place in the row, place in its load); what is past the end comes as -infinity.  `each_load` hands
+// whole loads to f(16 bytes, place of their first element, how many of them are another thread's): with MASK these
+// come as -infinity, without as they are.
+template <int W, int NV, typename T, bool MASK = true>
 struct HeldRow {
     u32x4 raw[NV];
-    unsigned int first, last;   // the thread's first element; where the row's last load starts
+    static constexpr bool kHeld = true;
+    unsigned int begin, first, last;   // the piece's first element and the thread's; where the last load starts
     static constexpr unsigned int kStep = 64u * W * kPerLoad<T>;
     static constexpr unsigned int kMost = NV * kStep;
-    __device__ __forceinline__ HeldRow(const T* x, unsigned int begin, unsigned int end) {
+    __device__ __forceinline__ HeldRow(const Global<T>* x, unsigned int begin_, unsigned int end) {
+        begin = begin_;
         first = begin + threadIdx.x * kPerLoad<T>;
         last = end - kPerLoad<T>;
 #pragma unroll
         for (int v = 0; v < NV; ++v)
-            raw[v] = *reinterpret_cast<const u32x4_any*>(x + min(first + v * kStep, last));
+            raw[v] = *(const Global<u32x4_any>*)(x + min(first + v * kStep, last));
+        // (a branch that the whole workgroup takes: rows mostly fill their loads)
 #pragma unroll
-        for (int v = 0; v < NV; ++v) mask_moved<T>(raw[v], first + v * kStep, min(first + v * kStep, last));
+        for (int v = 0; v < NV; ++v)
+            if (MASK && begin + (v + 1) * kStep > end) mask_moved<T>(raw[v], first + v * kStep, min(first + v * kStep, last));
+    }
+    template <typename F>
+    __device__ __forceinline__ void each_load(F f) const {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if (v && last + kPerLoad<T> <= begin + v * kStep) continue;   // (nothing of the row)
+            u32x4 r = raw[v];
+            unsigned int i = first;
+            asm volatile("" : "+v"(r), "+v"(i));
+            i += v * kStep;
+            f(r, min(i, last), i - min(i, last));
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
@@ -87,19 +115,30 @@ struct HeldRow {
     }
 };
 
-// The same interface over memory, for rows that registers do not hold: every `each` reads the row again.
-template <int W, typename T>
+// The same interface over memory, for rows that registers do not hold: every pass reads the row again (and `each_load`
+// does not mask).
+template <int W, typename T, int UNROLL = 4>
 struct ReadRow {
-    const T* x;
+    static constexpr bool kHeld = false;
+    const Global<T>* x;
     unsigned int begin, end;
-    __device__ __forceinline__ ReadRow(const T* x_, unsigned int begin_, unsigned int end_) : x(x_), begin(begin_), end(end_) {}
+    __device__ __forceinline__ ReadRow(const Global<T>* x_, unsigned int begin_, unsigned int end_) : x(x_), begin(begin_), end(end_) {}
+    template <typename F>
+    __device__ __forceinline__ void each_load(F f) const {
+        constexpr unsigned int kStep = 64u * W * kPerLoad<T>;
+#pragma unroll UNROLL
+        for (unsigned int i = begin + threadIdx.x * kPerLoad<T>; i < end; i += kStep) {
+            const unsigned int at = load_place<T>(i, end);
+            f(*(const Global<u32x4_any>*)(x + at), at, i - at);
+        }
+    }
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
         constexpr unsigned int kStep = 64u * W * kPerLoad<T>;
-#pragma unroll 4
+#pragma unroll UNROLL
         for (unsigned int i = begin + threadIdx.x * kPerLoad<T>; i < end; i += kStep) {
             const unsigned int at = load_place<T>(i, end);
-            u32x4 raw = *reinterpret_cast<const u32x4_any*>(x + at);
+            u32x4 raw = *(const Global<u32x4_any>*)(x + at);
             mask_moved<T>(raw, i, at);
 #pragma unroll
             for (int e = 0; e < (int)kPerLoad<T>; ++e) f(element<T>(raw, e), at + e, e);

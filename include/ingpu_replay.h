@@ -327,8 +327,10 @@ rp_status inram_get_state(inram_replay_t* h, uint64_t* head, uint64_t* size, uin
  * Operators on rows of logits: what a program does with a network's output rows besides training on
  * them by temporal differences.  A row holds one logit per action; a Q-value serves as one
  * (softmax over Q / temperature is Boltzmann exploration).  They take any rows the caller has, of
- * 1 to 262,144 actions, keep no state, allocate nothing and may be captured into a graph.
- * Two calls that may overlap in time (two streams, two captured graphs) need a workspace each.
+ * 1 to 262,144 actions, keep no state, allocate nothing and may be captured into a graph.  A workspace is
+ * device memory, 256-byte aligned, of at least the size that the call's *_workspace_bytes gives (it may be NULL
+ * where that is 0; RP_ENOMEM if it is too small); nothing in it has to be kept or cleared between
+ * calls.  Two calls that may overlap in time (two streams, two captured graphs) need one each.
  */
 typedef struct {
     const void* data;     /* device: element (i, j) is data[i * stride + j], aligned to its type */

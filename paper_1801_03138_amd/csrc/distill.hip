@@ -241,7 +241,8 @@ __device__ __forceinline__ double quarter_sum(double v) {
 // the teacher's to one maximum, with one exp for all, and one log serves for the logarithms too.
 template <bool REST>
 __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long long row, float weight, const EntryPart* part,
-                                           unsigned int parts, const MaxSum* rows, unsigned int pieces, RowScalars* out) {
+                                           unsigned int parts, const MaxSum* rows, unsigned int pieces, RowScalars* out,
+                                           bool put_loss = true) {
     const unsigned int lane = threadIdx.x & 63u, quarter = lane >> 4, l = lane & 15u;
     const bool part_here = l < parts, row_here = l < pieces;
     const EntryPart& r = part[part_here ? l : 0u];
@@ -292,7 +293,7 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     const bool empty = !bad && (m == -INFINITY || (!REST && !any));
     if (bad) loss = NAN;
     if (lane == 0) {
-        p.loss[row] = empty ? 0.f : (float)(loss * (double)weight);
+        if (put_loss) p.loss[row] = empty ? 0.f : (float)(loss * (double)weight);
         const double scale = (double)weight * p.inv_ts;
         *out = RowScalars{m > -INFINITY ? m : 0.f, bad ? NAN : (float)(scale * outside / total), shift, q_scale, inside, scale,
                           1.0 / total, empty ? 1u : bad ? 2u : 0u};
@@ -480,10 +481,135 @@ __global__ __launch_bounds__(64 * W, EU) void distill_kernel(DistillArgs p) {
     }
 }
 
+// ------------------------------------------------------------------------------------- few long rows, in pieces
+// A row in up to 64 pieces of a workgroup each: one launch for the pieces' maxima and sums, one that joins them and writes
+// the pieces' gradients.  The first also fetches the student's logits of the entries, since the second may overwrite them.
+struct Pieces {
+    unsigned int count, length;   // of a row; the last piece takes what is left
+};
+struct PieceSum {
+    MaxSum sum;
+    unsigned int twice, pad_;
+};
+static_assert(sizeof(PieceSum) == 24, "as the workspace is counted");
+
+Pieces pieces_of(unsigned long long rows, unsigned int n) {
+    // Where a workgroup a row leaves most of the 256 compute units idle and a row takes one of them longer than a second launch
+    // does (about 5 us): up to 128 rows of more than 32,768 actions, 32 rows of more than 16,384.  One workgroup a
+    // row -> pieces, us: 11 x 131071 fp32 44 -> 17, 128 x 50000 fp32 30 -> 27 (its loss alone 27 -> 18), 128 x 100000 bf16
+    // 34 -> 30; beyond the limits 64 x 20000 fp32 13 -> 16, 128 x 32768 bf16 16 -> 18, 256 x 100000 bf16 37 -> 45.
+    if (rows > (n > 32768u ? 128u : 32u) || n <= 16384u) return Pieces{1u, n};
+    const unsigned int most = (unsigned int)((1024u + rows - 1u) / rows);
+    unsigned int count = n / 2048u;
+    count = count > most ? most : count;
+    count = count > 64u ? 64u : count;
+    const unsigned int length = (n / count + 63u) / 64u * 64u;
+    count = n / length;
+    return Pieces{count, length};
+}
+size_t pieces_bytes(unsigned long long rows, unsigned int n, unsigned int k) {
+    const Pieces c = pieces_of(rows, n);
+    return c.count == 1u ? 0 : align_up(rows * c.count * sizeof(PieceSum), 256) + align_up(rows * k * 4u, 256);
+}
+
+template <int W, typename T, typename TT, bool REST>
+__global__ __launch_bounds__(64 * W, 4) void distill_piece_kernel(DistillArgs p, Pieces c, PieceSum* sums, float* z) {
+    extern __shared__ unsigned int named[];
+    __shared__ MaxSum part[W];
+    __shared__ unsigned int twice;
+    const unsigned int tid = threadIdx.x, k = p.k, piece = blockIdx.x;
+    const unsigned long long row = blockIdx.y;
+    if ((p.weight ? global_in<float>(p.weight)[row] : 1.f) == 0.f) return;
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    const unsigned int begin = piece * c.length, end = piece + 1u == c.count ? p.x.n : begin + c.length;
+    for (unsigned int i = tid; i < (end - begin + 31u) / 32u + 1u; i += 64 * W) named[i] = 0;
+    if (tid == 0) twice = 0;
+    __syncthreads();
+    for (unsigned int e = tid; e < k; e += 64 * W) {
+        const unsigned int a = (unsigned int)global_in<int>(p.entry)[row * k + e];
+        if (a >= begin && a < end) {
+            const unsigned int at = a - begin, bit = 1u << (at & 31u);
+            if (atomicOr(&named[at >> 5], bit) & bit) twice = 1;
+            global_out<float>(z)[row * k + e] = logit_value(x + a);
+        }
+    }
+    __syncthreads();
+    const ReadRow<W, T> read(x, begin, end);
+    const MaxSum mine = sum_row<REST, T>(read, read, begin, named, p.c2);
+    if ((tid & 63u) == 0) part[tid >> 6] = mine;
+    __syncthreads();
+    if (tid == 0) {
+        float m = part[0].m;
+        for (int w = 1; w < W; ++w) m = fmaxf(m, part[w].m);
+        double sum = 0.0;
+        for (int w = 0; w < W; ++w)
+            if (!(part[w].s == 0.0)) sum += part[w].s * (part[w].m > -INFINITY ? exp(((double)part[w].m - (double)m) * p.inv_ts) : 1.0);
+        sums[row * c.count + piece] = PieceSum{MaxSum{m, sum}, twice, 0};
+    }
+}
+
+template <int W, typename T, typename TT, bool REST, bool GRAD>
+__global__ __launch_bounds__(64 * W, 4) void distill_join_kernel(DistillArgs p, Pieces c, const PieceSum* sums, const float* z) {
+    extern __shared__ unsigned int lds[];
+    __shared__ DistillShared<W> s;
+    const unsigned int tid = threadIdx.x, k = p.k, piece = blockIdx.x;
+    const unsigned long long row = blockIdx.y;
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
+    const unsigned int begin = piece * c.length, end = piece + 1u == c.count ? p.x.n : begin + c.length;
+    const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
+    if (weight == 0.f) {
+        if (tid == 0 && piece == 0) p.loss[row] = 0.f;
+        if (GRAD) put_zeros<W, T>(g + begin, end - begin);
+        return;
+    }
+    const Entries en{reinterpret_cast<int*>(lds), reinterpret_cast<float*>(lds + k), reinterpret_cast<float*>(lds + 2u * k)};
+    // (the pieces' sums, a lane each, as one)
+    float m = -INFINITY;
+    double sum = 0.0;
+    unsigned int twice = 0;
+    if (tid < c.count) {
+        const PieceSum& q = sums[row * c.count + tid];
+        m = q.sum.m;
+        sum = q.sum.s;
+        twice = q.twice;
+    }
+    load_entries<W, T, TT, false>(p, row, x, z, 0, 0, en, nullptr, s);
+    if (tid < 64) {
+        const float all = wave_reduce(m, MaxOp{});
+        if (!(sum == 0.0) && m > -INFINITY) sum *= exp(((double)m - (double)all) * p.inv_ts);
+        sum = wave_reduce(sum, SumOp{});
+        twice = __ballot(twice) != 0;
+        if (tid == 0) {
+            s.row[0] = MaxSum{all, sum};
+            s.twice = twice;
+        }
+    }
+    __syncthreads();
+    sum_entries<W, REST>(p, row, en, s);
+    __syncthreads();
+    if (tid < 64) finish_row<REST>(p, row, weight, s.part, W, s.row, 1, &s.out, piece == 0);
+    if (!GRAD) return;
+    __syncthreads();
+    put_gradient<T>(ReadRow<W, T>(x, begin, end), g, s.out, p.c2);
+    __syncthreads();   // (an action with an entry is written again)
+    if (s.out.state == 0) put_entries<W, T>(p, g, en, begin, end, s.out, s.twice != 0);
+}
+
 template <typename T, typename TT, bool REST, bool GRAD>
-hipError_t launch_rows(const DistillArgs& a, hipStream_t st) {
+hipError_t launch_rows(const DistillArgs& a, void* workspace, hipStream_t st) {
     const unsigned int n = a.x.n, blocks = (unsigned int)(a.x.rows < (1ull << 18) ? a.x.rows : (1ull << 18));
     const size_t lds = ((n + 31u) / 32u + 1u + 3u * a.k) * 4u;
+    const Pieces c = pieces_of(a.x.rows, n);
+    if (c.count > 1u) {
+        const unsigned int rows = (unsigned int)a.x.rows;
+        PieceSum* sums = static_cast<PieceSum*>(workspace);
+        float* z = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + align_up(rows * c.count * sizeof(PieceSum), 256));
+        const size_t marks = ((n - (c.count - 1u) * c.length + 31u) / 32u + 1u) * 4u;
+        distill_piece_kernel<4, T, TT, REST><<<dim3(c.count, rows), 256, marks, st>>>(a, c, sums, z);
+        distill_join_kernel<4, T, TT, REST, GRAD><<<dim3(GRAD ? c.count : 1u, rows), 256, 12u * a.k, st>>>(a, c, sums, z);
+        return hipGetLastError();
+    }
     if (n <= 256u) {
         distill_wave_kernel<4, T, TT, REST, GRAD><<<blocks, 64, (8u + 3u * a.k) * 4u, st>>>(a);
     } else if constexpr (!GRAD) {
@@ -499,13 +625,13 @@ hipError_t launch_rows(const DistillArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 template <typename T, typename TT>
-hipError_t launch_distill(const DistillArgs& a, bool gradient, hipStream_t st) {
-    if (a.teacher_lse) return gradient ? launch_rows<T, TT, true, true>(a, st) : launch_rows<T, TT, true, false>(a, st);
-    return gradient ? launch_rows<T, TT, false, true>(a, st) : launch_rows<T, TT, false, false>(a, st);
+hipError_t launch_distill(const DistillArgs& a, bool gradient, void* ws, hipStream_t st) {
+    if (a.teacher_lse) return gradient ? launch_rows<T, TT, true, true>(a, ws, st) : launch_rows<T, TT, true, false>(a, ws, st);
+    return gradient ? launch_rows<T, TT, false, true>(a, ws, st) : launch_rows<T, TT, false, false>(a, ws, st);
 }
 
 rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad,
-                  uint64_t grad_stride, bool gradient, void* hip_stream) {
+                  uint64_t grad_stride, bool gradient, void* workspace, size_t bytes, void* hip_stream) {
     const char* why = logit_rows_fault(logits);
     RP_REQUIRE(!why, "%s: %s", what, why);
     RP_REQUIRE(teacher, "%s: null teacher", what);
@@ -529,6 +655,11 @@ rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* tea
         RP_REQUIRE(a1 <= g0 || g1 <= a0 || (a0 == g0 && (logits->rows == 1 || logits->stride == grad_stride)),
                    "%s: the gradient overlaps the logits other than in place", what);
     }
+    const size_t need = pieces_bytes(logits->rows, logits->n, teacher->k);
+    if (const char* fault = workspace_fault(workspace, bytes, need)) {
+        set_error("%s: %s (%zu bytes given, %zu needed)", what, fault, bytes, need);
+        return RP_ENOMEM;
+    }
     const DistillArgs a{logit_rows(logits), static_cast<const unsigned char*>(teacher->value), teacher->index, teacher->lse,
                         teacher->weight, teacher->k, 1.0 / teacher->temperature, 1.0 / teacher->student_temperature,
                         (float)(1.4426950408889634 / teacher->student_temperature), loss,
@@ -536,8 +667,8 @@ rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* tea
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const bool xb = logits->dtype == RP_BF16, tb = teacher->dtype == RP_BF16;
     typedef unsigned short B;
-    RP_CHECK_HIP(xb ? (tb ? launch_distill<B, B>(a, gradient, st) : launch_distill<B, float>(a, gradient, st))
-                    : (tb ? launch_distill<float, B>(a, gradient, st) : launch_distill<float, float>(a, gradient, st)));
+    RP_CHECK_HIP(xb ? (tb ? launch_distill<B, B>(a, gradient, workspace, st) : launch_distill<B, float>(a, gradient, workspace, st))
+                    : (tb ? launch_distill<float, B>(a, gradient, workspace, st) : launch_distill<float, float>(a, gradient, workspace, st)));
     return RP_OK;
 }
 
@@ -553,21 +684,17 @@ size_t rp_distill_workspace_bytes(const rp_rows* logits, uint32_t k) {
         rp::set_error("rp_distill_workspace_bytes: %s", why);
         return (size_t)-1;
     }
-    return 0;
+    return rp::pieces_bytes(logits->rows, logits->n, k);
 }
 
 rp_status rp_distill_loss(const rp_rows* logits, const rp_teacher* teacher, float* loss, void* workspace, size_t bytes,
                           void* hip_stream) {
-    (void)workspace;
-    (void)bytes;
-    return rp::distill("rp_distill_loss", logits, teacher, loss, nullptr, 0, false, hip_stream);
+    return rp::distill("rp_distill_loss", logits, teacher, loss, nullptr, 0, false, workspace, bytes, hip_stream);
 }
 
 rp_status rp_distill_grad(const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad, uint64_t grad_stride,
                           void* workspace, size_t bytes, void* hip_stream) {
-    (void)workspace;
-    (void)bytes;
-    return rp::distill("rp_distill_grad", logits, teacher, loss, grad, grad_stride, true, hip_stream);
+    return rp::distill("rp_distill_grad", logits, teacher, loss, grad, grad_stride, true, workspace, bytes, hip_stream);
 }
 
 }  // extern "C"

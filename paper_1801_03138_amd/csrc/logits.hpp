@@ -218,6 +218,11 @@ inline const char* logit_data_fault(const rp_rows* r) {
     if (reinterpret_cast<uintptr_t>(r->data) & (r->dtype == RP_BF16 ? 1u : 3u)) return "logits not aligned to their type";
     return nullptr;
 }
+inline const char* workspace_fault(const void* workspace, size_t bytes, size_t need) {
+    if (need == 0) return nullptr;
+    if (!workspace || bytes < need) return "the workspace is too small";
+    return reinterpret_cast<uintptr_t>(workspace) & 255u ? "the workspace must be 256-byte aligned" : nullptr;
+}
 inline LogitRows logit_rows(const rp_rows* r) {
     return LogitRows{static_cast<const unsigned char*>(r->data), r->rows, r->stride, r->n};
 }

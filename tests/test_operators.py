@@ -123,3 +123,15 @@ def test_the_binding_checks_tensors():
     for bad in (torch.zeros(3), torch.zeros(4, dtype=torch.float64), torch.zeros(8)[::2]):
         with pytest.raises(ValueError):
             B.check_setting(bad, torch.float32, 4, cpu, "t")
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    lib = B.lib()
+    x = rows(rows=2, n=200_000, stride=200_000)
+    for need, call in ((lib.rp_distill_workspace_bytes(C.byref(x), 8),
+                        lambda ws, b: lib.rp_distill_loss(C.byref(x), C.byref(teacher()), P, ws, b, None)),
+                       (lib.rp_distill_workspace_bytes(C.byref(x), 8),
+                        lambda ws, b: lib.rp_distill_grad(C.byref(x), C.byref(teacher()), P, 0x10000000, 200_000, ws, b, None))):
+        assert need > 0
+        assert call(None, 0) == B.RP_ENOMEM and call(0x1000, need - 1) == B.RP_ENOMEM and call(None, need) == B.RP_ENOMEM
+        assert call(0x1010, need) == B.RP_ENOMEM and b"aligned" in lib.rp_last_error()

@@ -286,18 +286,24 @@ __device__ unsigned int gather_words(const Row& row, ChooseShared<W>& s, In in) 
     return taken;
 }
 
-template <int W, typename Row>
-__device__ float row_max(const Row& row, ChooseShared<W>& s) {
-    float m = -INFINITY;
-    row.each([&](float x, unsigned int, int) { m = fmaxf(m, x); });
+// The maximum of each of a thread's slots (its elements at one place of its loads), and the row's.
+template <int W, int SLOTS, typename Row>
+__device__ __forceinline__ float slot_max(const Row& row, float (&slot)[SLOTS], ChooseShared<W>& s) {
+#pragma unroll
+    for (int e = 0; e < SLOTS; ++e) slot[e] = -INFINITY;
+    row.each([&](float x, unsigned int, int e) { slot[e] = fmaxf(slot[e], x); });
+    float m = slot[0];
+#pragma unroll
+    for (int e = 1; e < SLOTS; ++e) m = fmaxf(m, slot[e]);
     m = wave_reduce(m, MaxOp{});
     float* part = reinterpret_cast<float*>(s.part);
-    __syncthreads();
-    if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = m;
-    __syncthreads();
+    if (W > 1) {
+        if ((threadIdx.x & 63u) == 0) part[threadIdx.x >> 6] = m;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < W; ++w) m = fmaxf(m, part[w]);
-    __syncthreads();
+        for (int w = 0; w < W; ++w) m = fmaxf(m, part[w]);
+        __syncthreads();
+    }
     return m + 0.f;
 }
 
@@ -328,16 +334,11 @@ __device__ __forceinline__ unsigned int bin_of_count(const unsigned int* counts,
     return __shfl(bin, (int)owner, 64);
 }
 
-// A value that the k largest of a row (maximum m) are not below, and not many more are not: the k-th largest of
-// the slices' maxima, to one of 1024 steps.  A slice is what a thread holds in one place of its loads, so the slices
-// are 64 W times 4 or 8, at least 1024.
-template <int W, int SLOTS>
-__device__ float top_threshold(const float (&slot)[SLOTS], float m, unsigned int k, ChooseShared<W>& s) {
+// A value that at least k of some numbers between `low` (each thread's own share of them) and m are not below, and not many
+// more: the k-th largest to one of 1024 steps.  `each` hands every one of the thread's numbers to what it is given.
+template <int W, typename Each>
+__device__ float threshold_of(float low, float m, unsigned int k, ChooseShared<W>& s, Each each) {
     const unsigned int tid = threadIdx.x;
-    float low = INFINITY;
-#pragma unroll
-    for (int e = 0; e < SLOTS; ++e)
-        if (slot[e] > -INFINITY) low = fminf(low, slot[e]);
     low = wave_reduce(low, MinOp{});
     float* part = reinterpret_cast<float*>(s.part);
     __syncthreads();
@@ -348,10 +349,7 @@ __device__ float top_threshold(const float (&slot)[SLOTS], float m, unsigned int
     for (int w = 0; w < W; ++w) low = fminf(low, part[w]);
     const float range = m - low;
     const float scale = range > 0.f && range < INFINITY ? (kSliceBins - 1) / range : 0.f;
-#pragma unroll
-    for (int e = 0; e < SLOTS; ++e)
-        if (slot[e] > -INFINITY)
-            atomicAdd(&s.slices[min((unsigned int)((m - slot[e]) * scale), kSliceBins - 1u)], 1u);
+    each([&](float v) { atomicAdd(&s.slices[min((unsigned int)((m - v) * scale), kSliceBins - 1u)], 1u); });
     __syncthreads();
     if (tid < 64) {
         const unsigned int b = bin_of_count(s.slices, kSliceBins, k);
@@ -368,15 +366,19 @@ __device__ float top_threshold(const float (&slot)[SLOTS], float m, unsigned int
     return s.key;
 }
 
-// The first k and perhaps more of the row, sorted; returns how many, or more than kList if they do not fit.
-template <int W, int SLOTS, typename Row>
-__device__ unsigned int top_words(const Row& row, float m, unsigned int k, ChooseShared<W>& s) {
-    float slot[SLOTS];
+// A value that the k largest of a row (maximum m) are not below, and not many more are not, from the slices' maxima.  A slice
+// is what a thread holds in one slot, so there are 64 W times 4 or 8 of them, at least 1024.
+template <int W, int SLOTS>
+__device__ __forceinline__ float top_threshold(const float (&slot)[SLOTS], float m, unsigned int k, ChooseShared<W>& s) {
+    float low = INFINITY;
 #pragma unroll
-    for (int e = 0; e < SLOTS; ++e) slot[e] = -INFINITY;
-    row.each([&](float x, unsigned int, int e) { slot[e] = fmaxf(slot[e], x); });
-    const float t = top_threshold<W, SLOTS>(slot, m, k, s);
-    return gather_words<W>(row, s, [&](float x) { return x >= t; });
+    for (int e = 0; e < SLOTS; ++e)
+        if (slot[e] > -INFINITY) low = fminf(low, slot[e]);
+    return threshold_of<W>(low, m, k, s, [&](auto count) {
+#pragma unroll
+        for (int e = 0; e < SLOTS; ++e)
+            if (slot[e] > -INFINITY) count(slot[e]);
+    });
 }
 
 // ---------------------------------------------------------------------------------- sums along a sorted list
@@ -679,7 +681,8 @@ __device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned 
 template <int W, int SLOTS, typename T, typename Row>
 __device__ void choose_row(const Row& held, const ChooseArgs& p, unsigned long long row, ChooseShared<W>& s) {
     const RowChoice c = row_choice(p, row);
-    const float m = row_max<W>(held, s);
+    float slot[SLOTS];
+    const float m = slot_max<W, SLOTS>(held, slot, s);
     if (m == -INFINITY) {
         if (threadIdx.x == 0) put_choice(p, row, -1, 0.f);
         return;
@@ -687,7 +690,8 @@ __device__ void choose_row(const Row& held, const ChooseArgs& p, unsigned long l
     bool done = false;
     if (!c.search && !(m == INFINITY)) {
         if (c.k) {
-            const unsigned int count = top_words<W, SLOTS>(held, m, c.k, s);
+            const float t = top_threshold<W, SLOTS>(slot, m, c.k, s);
+            const unsigned int count = gather_words<W>(held, s, [&](float x) { return x >= t; });
             if (count <= kList) {
                 sort_words<W>(s.words, count);
                 if (threadIdx.x < 64) choose_from_list(p, row, c, s.words, count, m, s.sums);
@@ -706,20 +710,14 @@ __device__ void choose_row(const Row& held, const ChooseArgs& p, unsigned long l
     }
 }
 
-template <int W, int NV, typename T>
-__global__ __launch_bounds__(64 * W) void choose_kernel(ChooseArgs p) {
+template <int W, int NV, int EU, typename T>
+__global__ __launch_bounds__(64 * W, EU) void choose_kernel(ChooseArgs p) {
     __shared__ ChooseShared<W> s;
-    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
-        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
-        __syncthreads();
-        if constexpr (NV > 0) {
-            const HeldRow<W, NV, T> held(x, 0, p.x.n);
-            choose_row<W, (int)kPerLoad<T>, T>(held, p, row, s);
-        } else {
-            const ReadRow<W, T> read(x, 0, p.x.n);
-            choose_row<W, (int)kPerLoad<T>, T>(read, p, row, s);
-        }
-    }
+    const unsigned long long row = workgroup_row();
+    if (row >= p.x.rows) return;
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    const HeldRow<W, NV, T> held(x, 0, p.x.n);
+    choose_row<W, (int)kPerLoad<T>, T>(held, p, row, s);
 }
 
 // -------------------------------------------------------------------------------------------- top actions
@@ -767,48 +765,55 @@ __device__ unsigned int top_by_search(const Global<T>* x, unsigned int n, unsign
     return k;
 }
 
+// The sum of exp((x - m) / temperature) over what the workgroup holds, in every thread.  (The sum of a load in 32 bits, sums of
+// those in 64.)
+template <int W, int SLOTS, typename Row>
+__device__ __forceinline__ double exp_sum(const Row& held, float m, float c2, ChooseShared<W>& s) {
+    double a = 0.0;
+    if (m > -INFINITY && m < INFINITY) {
+        float load = 0.f;
+        held.each([&](float v, unsigned int, int e) {
+            const float w = __builtin_amdgcn_exp2f((fmaxf(v, -INFINITY) - m) * c2);
+            load = e ? load + w : w;
+            if (e == SLOTS - 1) a += (double)load;
+        });
+    }
+    a = block_reduce<W>(a, SumOp{}, s.part);
+    __syncthreads();
+    return a;
+}
+__device__ __forceinline__ void put_lse(const TopArgs& p, unsigned long long row, float m, double total) {
+    p.lse[row] = m == INFINITY || m == -INFINITY ? m : (float)((double)m * p.inv_t + log(total));
+}
+
 template <int W, int SLOTS, typename T, typename Row>
 __device__ void top_row(const Row& held, const TopArgs& p, unsigned long long row, const Global<T>* x, ChooseShared<W>& s) {
-    const float m = row_max<W>(held, s);
-    if (p.lse) {
-        // (the sum of a load in 32 bits, sums of those in 64)
-        double a = 0.0;
-        if (m > -INFINITY && m < INFINITY) {
-            float load = 0.f;
-            held.each([&](float v, unsigned int, int e) {
-                const float w = __builtin_amdgcn_exp2f((fmaxf(v, -INFINITY) - m) * p.c2);
-                load = e ? load + w : w;
-                if (e == SLOTS - 1) a += (double)load;
-            });
-        }
-        const double total = block_reduce<W>(a, SumOp{}, s.part);
-        if (threadIdx.x == 0)
-            p.lse[row] = m == INFINITY || m == -INFINITY ? m : (float)((double)m * p.inv_t + log(total));
-        __syncthreads();
-    }
+    float slot[SLOTS];
+    const float m = slot_max<W, SLOTS>(held, slot, s);
     unsigned int count = 0;
     if (m > -INFINITY) {
-        count = top_words<W, SLOTS>(held, m, p.k, s);
+        const float t = top_threshold<W, SLOTS>(slot, m, p.k, s);
+        count = gather_words<W>(held, s, [&](float v) { return v >= t; });
+    }
+    if (p.lse) {
+        const double total = exp_sum<W, SLOTS>(held, m, p.c2, s);
+        if (threadIdx.x == 0) put_lse(p, row, m, total);
+    }
+    if (m > -INFINITY) {
         if (count > kList) count = top_by_search<W, T>(x, p.x.n, p.k, m, s);
         sort_words<W>(s.words, count);
     }
     put_top<W, T>(p, row, s.words, min(count, p.k));
 }
 
-template <int W, int NV, typename T>
-__global__ __launch_bounds__(64 * W) void top_kernel(TopArgs p) {
+template <int W, int NV, int EU, typename T>
+__global__ __launch_bounds__(64 * W, EU) void top_kernel(TopArgs p) {
     __shared__ ChooseShared<W> s;
-    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
-        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
-        __syncthreads();
-        if constexpr (NV > 0) {
-            const HeldRow<W, NV, T> held(x, 0, p.x.n);
-            top_row<W, (int)kPerLoad<T>, T>(held, p, row, x, s);
-        } else {
-            const ReadRow<W, T> read(x, 0, p.x.n);
-            top_row<W, (int)kPerLoad<T>, T>(read, p, row, x, s);
-        }
-    }
+    const unsigned long long row = workgroup_row();
+    if (row >= p.x.rows) return;
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    const HeldRow<W, NV, T> held(x, 0, p.x.n);
+    top_row<W, (int)kPerLoad<T>, T>(held, p, row, x, s);
 }
 
 // ------------------------------------------------------------------- rows of up to 64 actions: one wavefront each
@@ -833,7 +838,9 @@ template <typename T>
 __global__ __launch_bounds__(256) void choose_wave_kernel(ChooseArgs p) {
     const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
     const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (unsigned long long row = blockIdx.x * 4ull + wave; row < p.x.rows; row += gridDim.x * 4ull) {
+    const unsigned long long row = workgroup_row() * 4u + wave;
+    if (row >= p.x.rows) return;
+    {
         const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
         const RowChoice c = row_choice(p, row);
@@ -844,11 +851,11 @@ __global__ __launch_bounds__(256) void choose_wave_kernel(ChooseArgs p) {
         const float m = wave_reduce(v, MaxOp{});
         if (m == -INFINITY) {
             if (lane == 0) put_choice(p, row, -1, 0.f);
-            continue;
+            return;
         }
         if (c.greedy) {
             if (rank == 0) put_choice(p, row, (int)lane, 0.f);
-            continue;
+            return;
         }
         const double w = allowed && (k <= 0 || (long long)rank < k) ? exp(-logit_depth(m, v, c.inv_t)) : 0.0;
         double before = 0.0, total = 0.0;
@@ -876,7 +883,9 @@ template <typename T>
 __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs p) {
     const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
     const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (unsigned long long row = blockIdx.x * 4ull + wave; row < p.x.rows; row += gridDim.x * 4ull) {
+    const unsigned long long row = workgroup_row() * 4u + wave;
+    if (row >= p.x.rows) return;
+    {
         const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
         const unsigned int rank = __popcll(lanes_before(order_key(v), n));
@@ -895,29 +904,289 @@ __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs p) {
     }
 }
 
-// ------------------------------------------------------------------------------------------------ launches
-// Workgroups of a launch: a row each, more rows than 2^18 in turn.
-unsigned int row_blocks(unsigned long long rows) { return (unsigned int)(rows < (1ull << 18) ? rows : (1ull << 18)); }
+// ------------------------------------------------------------------------------ rows in pieces of a workgroup each
+// Long rows, and few ones: a launch brings each piece of a row to its candidates or to its histogram of weights, in the
+// workspace; a second one, a workgroup a row, joins them.
+struct Pieces {
+    unsigned int count, length;   // of a row; the last piece takes what is left
+};
+struct PieceHead {
+    double top, sum;      // number of the histogram's first bin; sum of exp((x - m) / temperature)
+    float m;
+    unsigned int taken;   // candidates; more than kList: they did not fit
+    unsigned int pad_[2];
+};
+static_assert(sizeof(PieceHead) == 32, "as the workspace is counted");
+struct PieceSpace {
+    PieceHead* heads;                 // [rows][count]
+    unsigned long long* words;        // [rows][count][kList]: candidates, or the histogram
+};
+static_assert(kList == kBins, "candidates and histogram share their place");
 
-// A row goes to the smallest workgroup whose registers hold it; longer ones are read again for every pass.
+// One piece's elements at least a threshold that its k largest reach, as words in memory.
+template <int W, int SLOTS, typename Row>
+__device__ __forceinline__ unsigned int piece_words(const Row& held, const float (&slot)[SLOTS], float m, unsigned int k,
+                                                    unsigned long long* out, ChooseShared<W>& s) {
+    const float t = top_threshold<W, SLOTS>(slot, m, k, s);
+    if (threadIdx.x == 0) s.taken = 0;
+    __syncthreads();
+    held.each([&](float x, unsigned int i, int) {
+        if (x >= t) {
+            const unsigned int at = atomicAdd(&s.taken, 1u);
+            if (at < kList) global_out<unsigned long long>(out)[at] = order_word(logit_key(x), i);
+        }
+    });
+    __syncthreads();
+    return s.taken;
+}
+
+template <int W, int NV, int EU, typename T>
+__global__ __launch_bounds__(64 * W, EU) void choose_piece_kernel(ChooseArgs p, Pieces c, PieceSpace ws) {
+    constexpr int SLOTS = (int)kPerLoad<T>;
+    __shared__ ChooseShared<W> s;
+    const unsigned long long row = blockIdx.y, at = row * c.count + blockIdx.x;
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    const unsigned int begin = blockIdx.x * c.length, end = blockIdx.x + 1u == c.count ? p.x.n : begin + c.length;
+    const HeldRow<W, NV, T> held(x, begin, end);
+    const RowChoice choice = row_choice(p, row);
+    float slot[SLOTS];
+    const float m = slot_max<W, SLOTS>(held, slot, s);
+    unsigned int taken = 0;
+    double top = 0.0;
+    if (m > -INFINITY && m < INFINITY && !choice.search) {
+        unsigned long long* out = ws.words + at * kList;
+        if (choice.k) {
+            taken = piece_words<W, SLOTS>(held, slot, m, choice.k, out, s);
+        } else {
+            const Bins bins(m, choice.inv_t);
+            bin_weights<W>(held, bins, s);
+            for (unsigned int i = threadIdx.x; i < kBins; i += 64 * W) global_out<unsigned long long>(out)[i] = s.hist[i];
+            top = bins.top;
+        }
+    }
+    if (threadIdx.x == 0) ws.heads[at] = PieceHead{top, 0.0, m, taken, {0, 0}};
+}
+
+template <int W, int NV, int EU, typename T>
+__global__ __launch_bounds__(64 * W, EU) void top_piece_kernel(TopArgs p, Pieces c, PieceSpace ws) {
+    constexpr int SLOTS = (int)kPerLoad<T>;
+    __shared__ ChooseShared<W> s;
+    const unsigned long long row = blockIdx.y, at = row * c.count + blockIdx.x;
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    const unsigned int begin = blockIdx.x * c.length, end = blockIdx.x + 1u == c.count ? p.x.n : begin + c.length;
+    const HeldRow<W, NV, T> held(x, begin, end);
+    float slot[SLOTS];
+    const float m = slot_max<W, SLOTS>(held, slot, s);
+    unsigned int taken = 0;
+    if (m > -INFINITY) taken = piece_words<W, SLOTS>(held, slot, m, p.k, ws.words + at * kList, s);
+    __syncthreads();
+    const double sum = p.lse ? exp_sum<W, SLOTS>(held, m, p.c2, s) : 0.0;
+    if (threadIdx.x == 0) ws.heads[at] = PieceHead{0.0, sum, m, taken, {0, 0}};
+}
+
+// The candidates of a row's pieces (up to 64) as a sorted list in LDS of which the first k are the row's; returns its length, or
+// more than kList if they do not fit.  m: the row's maximum.
+template <int W>
+__device__ unsigned int join_words(const PieceHead* heads, const unsigned long long* words, unsigned int pieces, float m,
+                                   unsigned int k, ChooseShared<W>& s) {
+    const unsigned int tid = threadIdx.x, lane = tid & 63u;
+    const unsigned int mine = lane < pieces ? heads[lane].taken : 0u;
+    if (__ballot(mine > kList)) return kList + 1u;
+    const unsigned int total = wave_reduce(mine, SumOp{});
+    auto each_word = [&](auto f) {
+#pragma unroll 1
+        for (unsigned int q = 0; q < pieces; ++q) {
+            const unsigned int n = __shfl(mine, (int)q, 64);
+            for (unsigned int i = tid; i < n; i += 64 * W) f(global_in<unsigned long long>(words)[(size_t)q * kList + i]);
+        }
+    };
+    float t = -3.402823466e38f;
+    if (total > 128u && total > k) {
+        // the k-th largest to one of 1024 steps between the maximum and the smallest candidate
+        float low = INFINITY;
+        each_word([&](unsigned long long w) { low = fminf(low, key_value(word_key(w))); });
+        t = threshold_of<W>(low, m, k, s, [&](auto count) { each_word([&](unsigned long long w) { count(key_value(word_key(w))); }); });
+    }
+    if (tid == 0) s.taken = 0;
+    __syncthreads();
+    each_word([&](unsigned long long w) {
+        if (key_value(word_key(w)) >= t) {
+            const unsigned int at = atomicAdd(&s.taken, 1u);
+            if (at < kList) s.words[at] = w;
+        }
+    });
+    __syncthreads();
+    const unsigned int taken = s.taken;
+    __syncthreads();
+    if (taken <= kList) sort_words<W>(s.words, taken);
+    return taken;
+}
+
+template <int W, typename T>
+__global__ __launch_bounds__(64 * W, 4) void choose_join_kernel(ChooseArgs p, Pieces c, PieceSpace ws) {
+    __shared__ ChooseShared<W> s;
+    const unsigned int tid = threadIdx.x, lane = tid & 63u;
+    const unsigned long long row = blockIdx.x;
+    const PieceHead* heads = ws.heads + row * c.count;
+    const unsigned long long* words = ws.words + row * c.count * kList;
+    const RowChoice choice = row_choice(p, row);
+    const float m = wave_reduce(lane < c.count ? heads[lane].m : -INFINITY, MaxOp{});
+    if (m == -INFINITY) {
+        if (tid == 0) put_choice(p, row, -1, 0.f);
+        return;
+    }
+    bool done = false;
+    if (!choice.search && m < INFINITY) {
+        if (choice.k) {
+            const unsigned int count = join_words<W>(heads, words, c.count, m, choice.k, s);
+            if (count <= kList) {
+                if (tid < 64) choose_from_list(p, row, choice, s.words, count, m, s.sums);
+                done = true;
+            }
+        } else {
+            const Bins bins(m, choice.inv_t);
+            unsigned long long sum[kBins / (64 * W)] = {};
+#pragma unroll 1
+            for (unsigned int q = 0; q < c.count; ++q) {
+                const double down = bins.top - heads[q].top;   // bins between the row's first and the piece's
+                if (heads[q].m == -INFINITY || !(down < (double)kBins)) continue;
+                const unsigned int d = (unsigned int)down;
+#pragma unroll
+                for (unsigned int j = 0; j < kBins / (64 * W); ++j) {
+                    const unsigned int b = j * 64 * W + tid;
+                    if (b >= d) sum[j] += global_in<unsigned long long>(words)[(size_t)q * kBins + b - d];
+                }
+            }
+#pragma unroll
+            for (unsigned int j = 0; j < kBins / (64 * W); ++j) s.hist[j * 64 * W + tid] = sum[j];
+            __syncthreads();
+            sum_bins<W>(bins, m, s);
+            done = choose_from_bins<W>(ReadRow<W, T>(global_in<T>(p.x.data) + row * p.x.stride, 0, p.x.n), p, row, choice, bins, m, s);
+        }
+    }
+    if (!done) {
+        __syncthreads();
+        choose_by_search<W, T>(p, row, s.search);
+    }
+}
+
+template <int W, typename T>
+__global__ __launch_bounds__(64 * W, 4) void top_join_kernel(TopArgs p, Pieces c, PieceSpace ws) {
+    __shared__ ChooseShared<W> s;
+    const unsigned int lane = threadIdx.x & 63u;
+    const unsigned long long row = blockIdx.x;
+    const PieceHead* heads = ws.heads + row * c.count;
+    const float own = lane < c.count ? heads[lane].m : -INFINITY, m = wave_reduce(own, MaxOp{});
+    if (p.lse && threadIdx.x < 64) {
+        const double sum = own > -INFINITY && m < INFINITY ? heads[lane].sum * exp(-logit_depth(m, own, p.inv_t)) : 0.0;
+        const double total = wave_reduce(sum, SumOp{});
+        if (lane == 0) put_lse(p, row, m, total);
+    }
+    unsigned int count = 0;
+    if (m > -INFINITY) {
+        count = join_words<W>(heads, ws.words + row * c.count * kList, c.count, m, p.k, s);
+        if (count > kList) {
+            count = top_by_search<W, T>(global_in<T>(p.x.data) + row * p.x.stride, p.x.n, p.k, m, s);
+            sort_words<W>(s.words, count);
+        }
+    }
+    put_top<W, T>(p, row, s.words, min(count, p.k));
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+// How a row is cut: not at all where a workgroup's registers hold it and there are enough rows to fill the compute units.
 template <typename T>
-hipError_t launch_choose(const ChooseArgs& a, hipStream_t st) {
-    const unsigned int n = a.x.n, blocks = row_blocks(a.x.rows);
-    if (n <= 64u) choose_wave_kernel<T><<<row_blocks((a.x.rows + 3) / 4), 256, 0, st>>>(a);
-    else if (n <= HeldRow<4, 2, T>::kMost) choose_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
-    else if (n <= HeldRow<8, 8, T>::kMost) choose_kernel<8, 8, T><<<blocks, 512, 0, st>>>(a);
-    else if (n <= HeldRow<16, 16, T>::kMost) choose_kernel<16, 16, T><<<blocks, 1024, 0, st>>>(a);
-    else choose_kernel<16, 0, T><<<blocks, 1024, 0, st>>>(a);
+Pieces pieces_of(unsigned long long rows, unsigned int n) {
+    const unsigned int held = HeldRow<8, 8, T>::kMost;
+    if (n <= held && (rows > 128u || n <= 8192u)) return Pieces{1u, n};
+    // pieces as long as a workgroup holds; shorter ones down to 4096 while there are fewer than 512
+    unsigned int count = (n + held - 1u) / held;
+    const unsigned int fill = (unsigned int)((512u + rows - 1u) / rows), most = n / 4096u;
+    if (count < fill) count = fill < most ? fill : most > count ? most : count;
+    if (count > 64u) count = 64u;
+    const unsigned int length = (n / count + 63u) / 64u * 64u;
+    // (the last piece takes what is left, so it must fit too)
+    count = n / length;
+    if (n - (count - 1u) * length > held) ++count;
+    return Pieces{count, length};
+}
+Pieces pieces_of(const rp_rows* r) {
+    return r->dtype == RP_BF16 ? pieces_of<unsigned short>(r->rows, r->n) : pieces_of<float>(r->rows, r->n);
+}
+// Rows whose pieces are in the workspace at once (more go in several launches).
+unsigned long long rows_at_once(const rp_rows* r, const Pieces& c) {
+    const unsigned long long most = 8192u / c.count;
+    return r->rows < most ? r->rows : most;
+}
+size_t pieces_bytes(const rp_rows* r) {
+    if (r->rows == 0 || r->n <= 64u) return 0;
+    const Pieces c = pieces_of(r);
+    if (c.count == 1u) return 0;
+    const size_t n = rows_at_once(r, c) * c.count;
+    return align_up(n * sizeof(PieceHead), 256) + n * kList * 8u;
+}
+PieceSpace piece_space(void* workspace, unsigned long long rows, const Pieces& c) {
+    return PieceSpace{static_cast<PieceHead*>(workspace),
+                      reinterpret_cast<unsigned long long*>(static_cast<unsigned char*>(workspace) +
+                                                            align_up(rows * c.count * sizeof(PieceHead), 256))};
+}
+
+template <typename T>
+hipError_t launch_choose(const rp_rows* r, ChooseArgs a, void* workspace, hipStream_t st) {
+    const unsigned int n = a.x.n;
+    const dim3 blocks = row_grid(a.x.rows);
+    if (n <= 64u) {
+        choose_wave_kernel<T><<<row_grid((a.x.rows + 3) / 4), 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const Pieces c = pieces_of(r);
+    if (c.count == 1u) {
+        if (n <= HeldRow<4, 2, T>::kMost) choose_kernel<4, 2, 4, T><<<blocks, 256, 0, st>>>(a);
+        else choose_kernel<8, 8, 4, T><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const unsigned long long rows = a.x.rows, step = rows_at_once(r, c);
+    const PieceSpace ws = piece_space(workspace, step, c);
+    for (unsigned long long at = 0; at < rows; at += step) {
+        const unsigned int part = (unsigned int)(rows - at < step ? rows - at : step);
+        choose_piece_kernel<8, 8, 4, T><<<dim3(c.count, part), 512, 0, st>>>(a, c, ws);
+        choose_join_kernel<8, T><<<part, 512, 0, st>>>(a, c, ws);
+        a.x.data += part * a.x.stride * sizeof(T);
+        a.u += part;
+        a.index += part;
+        if (a.logp) a.logp += part;
+        if (a.row_temperature) a.row_temperature += part;
+        if (a.row_top_p) a.row_top_p += part;
+        if (a.row_min_p) a.row_min_p += part;
+        if (a.row_top_k) a.row_top_k += part;
+    }
     return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_top(const TopArgs& a, hipStream_t st) {
-    const unsigned int n = a.x.n, blocks = row_blocks(a.x.rows);
-    if (n <= 64u) top_wave_kernel<T><<<row_blocks((a.x.rows + 3) / 4), 256, 0, st>>>(a);
-    else if (n <= HeldRow<4, 2, T>::kMost) top_kernel<4, 2, T><<<blocks, 256, 0, st>>>(a);
-    else if (n <= HeldRow<8, 8, T>::kMost) top_kernel<8, 8, T><<<blocks, 512, 0, st>>>(a);
-    else if (n <= HeldRow<16, 16, T>::kMost) top_kernel<16, 16, T><<<blocks, 1024, 0, st>>>(a);
-    else top_kernel<16, 0, T><<<blocks, 1024, 0, st>>>(a);
+hipError_t launch_top(const rp_rows* r, TopArgs a, void* workspace, hipStream_t st) {
+    const unsigned int n = a.x.n;
+    const dim3 blocks = row_grid(a.x.rows);
+    if (n <= 64u) {
+        top_wave_kernel<T><<<row_grid((a.x.rows + 3) / 4), 256, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const Pieces c = pieces_of(r);
+    if (c.count == 1u) {
+        if (n <= HeldRow<4, 2, T>::kMost) top_kernel<4, 2, 4, T><<<blocks, 256, 0, st>>>(a);
+        else top_kernel<8, 8, 4, T><<<blocks, 512, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const unsigned long long rows = a.x.rows, step = rows_at_once(r, c);
+    const PieceSpace ws = piece_space(workspace, step, c);
+    for (unsigned long long at = 0; at < rows; at += step) {
+        const unsigned int part = (unsigned int)(rows - at < step ? rows - at : step);
+        top_piece_kernel<8, 8, 4, T><<<dim3(c.count, part), 512, 0, st>>>(a, c, ws);
+        top_join_kernel<8, T><<<part, 512, 0, st>>>(a, c, ws);
+        a.x.data += part * a.x.stride * sizeof(T);
+        a.values += (size_t)part * a.k * sizeof(T);
+        a.index += (size_t)part * a.k;
+        if (a.lse) a.lse += part;
+    }
     return hipGetLastError();
 }
 
@@ -931,7 +1200,7 @@ size_t rp_choose_workspace_bytes(const rp_rows* logits) {
         rp::set_error("rp_choose_workspace_bytes: %s", why);
         return (size_t)-1;
     }
-    return 0;
+    return rp::pieces_bytes(logits);
 }
 
 rp_status rp_choose_actions(const rp_rows* logits, const rp_choice* how, const float* u, int32_t* index, float* logp,
@@ -943,12 +1212,16 @@ rp_status rp_choose_actions(const rp_rows* logits, const rp_choice* how, const f
     why = rp::logit_data_fault(logits);
     RP_REQUIRE(!why, "rp_choose_actions: %s", why);
     RP_REQUIRE(u && index, "rp_choose_actions: null array");
-    (void)workspace;
-    (void)bytes;
+    const size_t need = rp::pieces_bytes(logits);
+    if (const char* fault = rp::workspace_fault(workspace, bytes, need)) {
+        rp::set_error("rp_choose_actions: %s (%zu bytes given, %zu needed)", fault, bytes, need);
+        return RP_ENOMEM;
+    }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const rp::ChooseArgs a{rp::logit_rows(logits), how->temperature, how->top_p, how->min_p, how->top_k,
                            how->row_temperature, how->row_top_p, how->row_min_p, how->row_top_k, u, index, logp};
-    RP_CHECK_HIP(logits->dtype == RP_BF16 ? rp::launch_choose<unsigned short>(a, st) : rp::launch_choose<float>(a, st));
+    RP_CHECK_HIP(logits->dtype == RP_BF16 ? rp::launch_choose<unsigned short>(logits, a, workspace, st)
+                                           : rp::launch_choose<float>(logits, a, workspace, st));
     return RP_OK;
 }
 
@@ -959,7 +1232,7 @@ size_t rp_top_workspace_bytes(const rp_rows* logits, uint32_t k) {
         rp::set_error("rp_top_workspace_bytes: %s", why);
         return (size_t)-1;
     }
-    return 0;
+    return rp::pieces_bytes(logits);
 }
 
 rp_status rp_top_actions(const rp_rows* logits, uint32_t k, double temperature, void* values, int32_t* index, float* lse,
@@ -972,12 +1245,16 @@ rp_status rp_top_actions(const rp_rows* logits, uint32_t k, double temperature, 
     why = rp::logit_data_fault(logits);
     RP_REQUIRE(!why, "rp_top_actions: %s", why);
     RP_REQUIRE(values && index, "rp_top_actions: null array");
-    (void)workspace;
-    (void)bytes;
+    const size_t need = rp::pieces_bytes(logits);
+    if (const char* fault = rp::workspace_fault(workspace, bytes, need)) {
+        rp::set_error("rp_top_actions: %s (%zu bytes given, %zu needed)", fault, bytes, need);
+        return RP_ENOMEM;
+    }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const rp::TopArgs a{rp::logit_rows(logits), k, 1.0 / temperature, (float)(1.4426950408889634 / temperature),
                         static_cast<unsigned char*>(values), index, lse};
-    RP_CHECK_HIP(logits->dtype == RP_BF16 ? rp::launch_top<unsigned short>(a, st) : rp::launch_top<float>(a, st));
+    RP_CHECK_HIP(logits->dtype == RP_BF16 ? rp::launch_top<unsigned short>(logits, a, workspace, st)
+                                           : rp::launch_top<float>(logits, a, workspace, st));
     return RP_OK;
 }
 

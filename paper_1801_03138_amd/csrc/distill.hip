@@ -385,15 +385,16 @@ __global__ __launch_bounds__(64) void distill_wave_kernel(DistillArgs p) {
     unsigned int* named = lds;
     const Entries en{reinterpret_cast<int*>(lds + kWords), reinterpret_cast<float*>(lds + kWords + k),
                      reinterpret_cast<float*>(lds + kWords + 2u * k)};
-    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
+    const unsigned long long row = workgroup_row();
+    if (row >= p.x.rows) return;
+    {
         const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
         const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
-        __syncthreads();
         if (weight == 0.f) {
             if (lane == 0) p.loss[row] = 0.f;
             if (GRAD) put_zeros<1, T>(g, n);
-            continue;
+            return;
         }
         const ShortRow<NV, T> held(x, n);
         if (lane < kWords) named[lane] = 0;
@@ -419,7 +420,7 @@ __global__ __launch_bounds__(64) void distill_wave_kernel(DistillArgs p) {
         if (lane == 0) s.row[0] = MaxSum{m, sum};
         __syncthreads();
         finish_row<REST>(p, row, weight, s.part, 1, s.row, 1, &s.out);
-        if (!GRAD) continue;
+        if (!GRAD) return;
         __syncthreads();
         const RowScalars o = s.out;
         const float factor = o.state == 1u ? 0.f : o.factor;
@@ -465,11 +466,12 @@ __global__ __launch_bounds__(64 * W, EU) void distill_kernel(DistillArgs p) {
     const unsigned int words = (n + 31u) / 32u + 1u;
     const Entries en{reinterpret_cast<int*>(lds + words), reinterpret_cast<float*>(lds + words + k),
                      reinterpret_cast<float*>(lds + words + 2u * k)};
-    for (unsigned long long row = blockIdx.x; row < p.x.rows; row += gridDim.x) {
+    const unsigned long long row = workgroup_row();
+    if (row >= p.x.rows) return;
+    {
         const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
         Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
         const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
-        __syncthreads();   // (the row before is done with LDS)
         if (weight == 0.f) {
             if (threadIdx.x == 0) p.loss[row] = 0.f;
             if (GRAD) put_zeros<W, T>(g, n);
@@ -598,7 +600,8 @@ __global__ __launch_bounds__(64 * W, 4) void distill_join_kernel(DistillArgs p, 
 
 template <typename T, typename TT, bool REST, bool GRAD>
 hipError_t launch_rows(const DistillArgs& a, void* workspace, hipStream_t st) {
-    const unsigned int n = a.x.n, blocks = (unsigned int)(a.x.rows < (1ull << 18) ? a.x.rows : (1ull << 18));
+    const unsigned int n = a.x.n;
+    const dim3 blocks = row_grid(a.x.rows);
     const size_t lds = ((n + 31u) / 32u + 1u + 3u * a.k) * 4u;
     const Pieces c = pieces_of(a.x.rows, n);
     if (c.count > 1u) {

@@ -204,6 +204,14 @@ __device__ __forceinline__ V block_reduce(V v, Op op, V* part) {
     return all;
 }
 
+// A workgroup a row, in several rows of workgroups where one would have 2^32 threads.  (A loop over rows in the kernel would
+// have the compiler keep what does not change from one to the next in the registers that the row needs.)
+__device__ __forceinline__ unsigned long long workgroup_row() { return (unsigned long long)blockIdx.y * gridDim.x + blockIdx.x; }
+inline dim3 row_grid(unsigned long long rows) {
+    const unsigned long long x = rows < (1ull << 16) ? rows : (1ull << 16);
+    return dim3((unsigned int)x, (unsigned int)((rows + x - 1) / x));
+}
+
 // Host side: rows that the kernels can be given, or why not.
 inline const char* logit_rows_fault(const rp_rows* r) {
     if (!r) return "null rows";

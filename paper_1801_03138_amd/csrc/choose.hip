@@ -203,6 +203,7 @@ __device__ __forceinline__ void store_value(Global<unsigned short>* p, float v) 
 constexpr unsigned int kBins = 2048;    // of the histogram of weights
 constexpr unsigned int kList = 2048;    // actions that are sorted in LDS
 constexpr unsigned int kSliceBins = 1024;
+constexpr unsigned int kBuckets = 1024, kFine = 256;
 
 template <int W>
 struct ChooseShared {
@@ -212,8 +213,14 @@ struct ChooseShared {
         unsigned int slices[kSliceBins];
     };
     unsigned long long words[kList];
+    union {
+        unsigned int buckets[kBuckets + 1];
+        unsigned long long fine[kFine];     // a bin's weights, by parts of the bin
+    };
     SearchShared<W> search;
     double part[W];
+    unsigned int wave_count[W];
+    unsigned long long word;
     unsigned int taken, bin;
     float key;
 };
@@ -224,12 +231,12 @@ __device__ __forceinline__ void wave_lds_fence() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Sorts `count` numbers in LDS (room for the next power of two), the largest first.  Up to 128: every
-// thread ranks one against all.  More: a bitonic network, where exchanges over less than 128 places stay within
-// the 128 numbers of one wavefront and need no barrier.
+// Sorts the `count` words in LDS, the largest first.  Up to 128: every thread ranks one against all.  More: 1024 buckets
+// linear in the value, a count of each, every word to its bucket's place, and there a rank against its bucket.
 template <int W>
-__device__ void sort_words(unsigned long long* w, unsigned int count) {
-    const unsigned int tid = threadIdx.x;
+__device__ void sort_words(ChooseShared<W>& s, unsigned int count) {
+    const unsigned int tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    unsigned long long* w = s.words;
     if (count <= 128u) {
         unsigned long long mine = 0;
         unsigned int rank = 0;
@@ -244,27 +251,80 @@ __device__ void sort_words(unsigned long long* w, unsigned int count) {
         __syncthreads();
         return;
     }
-    unsigned int padded = 256;
-    while (padded < count) padded <<= 1;
-    for (unsigned int i = count + tid; i < padded; i += 64 * W) w[i] = 0;
+    constexpr int kEach = kList / (64 * W), kPer = kBuckets / (64 * W);
+    unsigned long long mine[kEach];
+    unsigned int at[kEach];   // bucket << 16 | place in it
+    float low = INFINITY, high = -INFINITY;
     __syncthreads();
-#pragma unroll 1
-    for (unsigned int size = 2; size <= padded; size <<= 1)
-#pragma unroll 1
-        for (unsigned int gap = size >> 1; gap; gap >>= 1) {
-#pragma unroll 1
-            for (unsigned int t = tid; t < padded / 2u; t += 64 * W) {
-                const unsigned int i = 2u * t - (t & (gap - 1u)), j = i + gap;
-                const unsigned long long a = w[i], b = w[j];
-                if ((a < b) == ((i & size) == 0)) {
-                    w[i] = b;
-                    w[j] = a;
-                }
-            }
-            // (the next exchange is over gap / 2, or over `size` after the last of this size)
-            if (gap >= 128u || (gap == 1u && size >= 128u)) __syncthreads();
-            else wave_lds_fence();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const unsigned int i = j * 64 * W + tid;
+        mine[j] = i < count ? w[i] : 0ull;
+        if (i < count) {
+            low = fminf(low, key_value(word_key(mine[j])));
+            high = fmaxf(high, key_value(word_key(mine[j])));
         }
+    }
+    low = wave_reduce(low, MinOp{});
+    high = wave_reduce(high, MaxOp{});
+    float2* ends = reinterpret_cast<float2*>(s.part);
+    if (lane == 0) ends[wave] = float2{low, high};
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) s.buckets[j * 64 * W + tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < W; ++v) {
+        low = fminf(low, ends[v].x);
+        high = fmaxf(high, ends[v].y);
+    }
+    const float range = high - low, scale = range > 0.f && range < INFINITY ? (kBuckets - 1) / range : 0.f;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (j * 64 * W + tid < count) {
+            // (infinite ends share one bucket)
+            const unsigned int b = scale > 0.f ? min((unsigned int)((high - key_value(word_key(mine[j]))) * scale), kBuckets - 1u) : 0u;
+            at[j] = b << 16 | atomicAdd(&s.buckets[b], 1u);
+        }
+    __syncthreads();
+    // counts -> where each bucket starts
+    unsigned int c[kPer], run = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        c[j] = run;
+        run += s.buckets[tid * kPer + j];
+    }
+    unsigned int upto = run;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const unsigned int o = __shfl_up(upto, off, 64);
+        if (lane >= (unsigned int)off) upto += o;
+    }
+    if (lane == 63u) s.wave_count[wave] = upto;
+    __syncthreads();
+    unsigned int base = upto - run;
+#pragma unroll
+    for (int v = 0; v < W; ++v) base += (unsigned int)v < wave ? s.wave_count[v] : 0u;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) s.buckets[tid * kPer + j] = base + c[j];
+    if (tid == 0) s.buckets[kBuckets] = count;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (j * 64 * W + tid < count) w[s.buckets[at[j] >> 16] + (at[j] & 0xFFFFu)] = mine[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (j * 64 * W + tid < count) {
+            const unsigned int from = s.buckets[at[j] >> 16], to = s.buckets[(at[j] >> 16) + 1u];
+            unsigned int rank = from;
+#pragma unroll 1
+            for (unsigned int i = from; i < to; ++i) rank += w[i] > mine[j];
+            at[j] = rank;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (j * 64 * W + tid < count) w[at[j]] = mine[j];
     __syncthreads();
 }
 
@@ -501,6 +561,17 @@ struct Bins {
     }
 };
 
+// exp(z) 2^44 as a whole number, for z within +- 0.0195: the sixth power's term, which is left out, is below 2^-43.
+__device__ __forceinline__ unsigned long long near_units(double z) {
+    double w = fma(z, 1.0 / 120.0, 1.0 / 24.0);
+    w = fma(w, z, 1.0 / 6.0);
+    w = fma(w, z, 0.5);
+    w = fma(w, z, 1.0);
+    w = fma(w, z, 1.0);
+    // (adding 2^52 leaves the whole number in the low bits)
+    return __double_as_longlong(fma(w, kOne, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+}
+
 template <int W, typename Row>
 __device__ void bin_weights(const Row& row, const Bins& bins, ChooseShared<W>& s) {
     for (unsigned int i = threadIdx.x; i < kBins; i += 64 * W) s.hist[i] = 0;
@@ -510,16 +581,7 @@ __device__ void bin_weights(const Row& row, const Bins& bins, ChooseShared<W>& s
     row.each([&](float x, unsigned int, int) {
         if (x >= least) {
             const double at = (double)x * inv_width, whole = floor(at);
-            // exp of a number within +- 0.0195: the sixth power's term, which is left out, is below 2^-43
-            const double z = fma(at - whole, slope, -0.5 * slope);
-            double w = fma(z, 1.0 / 120.0, 1.0 / 24.0);
-            w = fma(w, z, 1.0 / 6.0);
-            w = fma(w, z, 0.5);
-            w = fma(w, z, 1.0);
-            w = fma(w, z, 1.0);
-            // (adding 2^52 leaves the whole number in the low bits)
-            const unsigned long long units = __double_as_longlong(fma(w, kOne, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
-            atomicAdd(&s.hist[(int)(top - whole)], units);
+            atomicAdd(&s.hist[(int)(top - whole)], near_units(fma(at - whole, slope, -0.5 * slope)));
         }
     });
     __syncthreads();
@@ -574,106 +636,163 @@ __device__ unsigned int find_bin(ChooseShared<W>& s, Reached reached) {
     return bin;
 }
 
-// From the inclusive sums over bins to the choice; false if a bin holds too many actions to be sorted.
+// The actions of bin b as words in LDS; false if they do not fit.
 template <int W, typename Row>
-__device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned long long row, const RowChoice& c,
-                                 const Bins& bins, float m, ChooseShared<W>& s) {
+__device__ bool list_bin(const Row& row, const Bins& bins, unsigned int b, ChooseShared<W>& s, unsigned int* count) {
+    const float lo = bins.lo((double)b), hi = bins.hi((double)b);
+    *count = gather_words<W>(row, s, [&](float x) { return x >= lo && x < hi; });
+    return *count <= kList;
+}
+
+// Of the `count` actions of bin b in LDS, the first in order with which the inclusive sum over the row reaches `target` (passes
+// it, if `past`), or the last of them if rounding has it otherwise: its word and that sum, in s.word and s.part[0].  A bin
+// holds some hundred actions of a long row, so a histogram of its parts comes before anything is sorted.
+template <int W>
+__device__ void locate(const Bins& bins, unsigned int b, unsigned int count, double target, bool past, float m, double inv_t,
+                       ChooseShared<W>& s) {
     const unsigned int tid = threadIdx.x;
-    double mass = s.sums[kBins - 1];
-    unsigned int have = kBins, count = 0, limit = 0xFFFFFFFFu;   // the bin whose sorted actions are in LDS, their number
-    auto list_bin = [&](unsigned int b) {
-        const float lo = bins.lo((double)b), hi = bins.hi((double)b);
-        count = gather_words<W>(row_, s, [&](float x) { return x >= lo && x < hi; });
-        if (count > kList) return false;
-        sort_words<W>(s.words, count);
-        have = b;
-        return true;
-    };
-    // the sum over the actions that stay
-    unsigned int last = kBins - 1;
-    const bool cut_p = c.top_p < 1.0, cut_m = c.min_p > 0.0;
-    if (cut_p || cut_m) {
-        unsigned int bin_p = kBins, bin_m = kBins;
-        // (the best action always stays, and the sum reaches its weight with it)
-        const double most = fmax(c.top_p * mass, 0.5);
-        if (cut_p) bin_p = find_bin<W>(s, [&](double v) { return v >= most; });
-        if (cut_m) {
-            const double b = bins.top - floor(((double)m + log(fmin(c.min_p, 1.0)) / c.inv_t) * bins.inv_width);
-            bin_m = b < (double)kBins ? (unsigned int)fmax(b, 0.0) : kBins;
-        }
-        last = min(bin_p, bin_m);
-        if (last < kBins) {
-            if (!list_bin(last)) return false;
-            const double before = last ? s.sums[last - 1u] : 0.0;
-            __syncthreads();
-            if (tid < 64) {
-                // walk the list 64 at a time: how many stay, and their sum
-                double run = before, kept = before;
-                unsigned int n = 0;
-#pragma unroll 1
-                for (unsigned int j0 = 0; j0 < count; j0 += 64) {
-                    const unsigned int j = j0 + tid;
-                    const double w = j < count ? exp(-logit_depth(m, key_value(word_key(s.words[j])), c.inv_t)) : 0.0;
-                    double v = w;
+    double before = b ? s.sums[b - 1u] : 0.0;
+    if (count > 128u) {
+        constexpr int kEach = kList / (64 * W);
+        unsigned long long mine[kEach];
+        unsigned int part[kEach];
+        for (unsigned int i = tid; i < kFine; i += 64 * W) s.fine[i] = 0;
+        __syncthreads();
 #pragma unroll
-                    for (int off = 1; off < 64; off <<= 1) {
-                        const double o = __shfl_up(v, off, 64);
-                        if (tid >= (unsigned int)off) v += o;
-                    }
-                    v += run;
-                    double prev = __shfl_up(v, 1, 64);
-                    if (tid == 0) prev = run;
-                    bool stays = j < count && (!cut_p || bin_p > last || prev < most) && (!cut_m || bin_m > last || w >= c.min_p);
-                    if (last == 0 && j == 0) stays = true;
-                    const unsigned long long yes = __ballot(stays);
-                    const unsigned int here = __popcll(yes);
-                    if (here) kept = __shfl(v, (int)here - 1, 64);
-                    n += here;
-                    run = __shfl(v, 63, 64);
-                    if (here < 64u) break;
-                }
-                if (tid == 0) {
-                    s.part[0] = kept;
-                    s.taken = n;
-                }
+        for (int j = 0; j < kEach; ++j) {
+            const unsigned int i = j * 64 * W + tid;
+            if (i < count) {
+                mine[j] = s.words[i];
+                const double at = (double)key_value(word_key(mine[j])) * bins.inv_width, rest = at - floor(at);
+                part[j] = min((unsigned int)((1.0 - rest) * kFine), kFine - 1u);
+                atomicAdd(&s.fine[part[j]], near_units(fma(rest, bins.slope, -0.5 * bins.slope)));
             }
-            __syncthreads();
-            mass = s.part[0];
-            limit = s.taken;
-            __syncthreads();
         }
+        __syncthreads();
+        if (tid < 64) {
+            constexpr int kPer = kFine / 64;
+            unsigned long long c[kPer], run = 0;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                c[j] = run;
+                run += s.fine[tid * kPer + j];
+            }
+            unsigned long long upto = run;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const unsigned long long o = __shfl_up(upto, off, 64);
+                if (tid >= (unsigned int)off) upto += o;
+            }
+            const double unit = bins.middle(m, (double)b) * (1.0 / kOne);
+            const unsigned long long start = upto - run;
+            // the first part that reaches the target, or the last one with anything in it
+            unsigned int first = kFine, last = 0;
+#pragma unroll
+            for (int j = kPer - 1; j >= 0; --j) {
+                const unsigned long long f = s.fine[tid * kPer + j];
+                const double v = before + (double)(start + c[j] + f) * unit;
+                if (f && (past ? v > target : v >= target)) first = tid * kPer + j;
+                if (f && !last) last = tid * kPer + j;
+            }
+            const unsigned int all = wave_reduce(first, MinOp{});
+            const unsigned int end = wave_reduce(last, MaxOp{});
+            const unsigned int take = all < kFine ? all : end;
+            if (tid == take / kPer) {
+                unsigned long long sum = start;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (tid * kPer + j < take) sum += s.fine[tid * kPer + j];
+                s.part[0] = before + (double)sum * unit;
+                s.bin = take;
+                s.taken = 0;
+            }
+        }
+        __syncthreads();
+        const unsigned int take = s.bin;
+        before = s.part[0];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if (j * 64 * W + tid < count && part[j] == take) s.words[atomicAdd(&s.taken, 1u)] = mine[j];
+        __syncthreads();
+        count = s.taken;
+        __syncthreads();
     }
-    // (nothing of the last bin may stay: the choice then lies in one before it)
-    const bool end = !(c.u < 1.f);
-    const double drawn = end ? mass : c.u > 0.f ? (double)c.u * mass : 0.0;
-    const unsigned int bin = min(find_bin<W>(s, [&](double v) { return end ? v >= drawn : v > drawn; }), last);
-    if (bin != have && !list_bin(bin)) return false;
-    const double before = bin ? s.sums[bin - 1u] : 0.0;
+    sort_words<W>(s, count);
     if (tid < 64) {
-        const unsigned int n = bin == last ? min(count, limit) : count;
-        double run = before;
-        unsigned int at = n ? n - 1u : 0u;
+        double run = before, sum = before;
+        unsigned int at = count - 1u;
+        bool found = false;
 #pragma unroll 1
-        for (unsigned int j0 = 0; j0 < n; j0 += 64) {
+        for (unsigned int j0 = 0; j0 < count && !found; j0 += 64) {
             const unsigned int j = j0 + tid;
-            double v = j < n ? exp(-logit_depth(m, key_value(word_key(s.words[j])), c.inv_t)) : 0.0;
+            double v = j < count ? exp(-logit_depth(m, key_value(word_key(s.words[j])), inv_t)) : 0.0;
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const double o = __shfl_up(v, off, 64);
                 if (tid >= (unsigned int)off) v += o;
             }
             v += run;
-            const unsigned long long yes = __ballot(j < n && (end ? v >= drawn : v > drawn));
-            if (yes) {
-                at = j0 + __ffsll((long long)yes) - 1u;
-                break;
-            }
             run = __shfl(v, 63, 64);
+            const unsigned long long yes = __ballot(j < count && (past ? v > target : v >= target));
+            found = yes != 0;
+            if (found) at = j0 + __ffsll((long long)yes) - 1u;
+            sum = found ? __shfl(v, (int)(at - j0), 64) : run;
         }
-        if (tid == 0)
-            put_choice(p, row, (int)word_index(s.words[at]),
-                       (float)(-logit_depth(m, key_value(word_key(s.words[at])), c.inv_t) - log(mass)));
+        if (tid == 0) {
+            s.word = s.words[at];
+            s.part[0] = sum;
+        }
     }
+    __syncthreads();
+}
+
+// From the inclusive sums over bins to the choice; false if a bin holds too many actions for LDS, or, by a rounding of the
+// sums, none.
+template <int W, typename Row>
+__device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned long long row, const RowChoice& c,
+                                 const Bins& bins, float m, ChooseShared<W>& s) {
+    const unsigned int tid = threadIdx.x;
+    double mass = s.sums[kBins - 1];
+    unsigned int count;
+    // the sum over the actions that stay: each limit keeps the first so many, and the shorter one counts
+    unsigned int bin_p = kBins, bin_m = kBins;
+    // (the best action always stays, and the sum reaches its weight with it)
+    const double most = fmax(c.top_p * mass, 0.5);
+    if (c.top_p < 1.0) bin_p = find_bin<W>(s, [&](double v) { return v >= most; });
+    if (c.min_p > 0.0) {
+        const double b = bins.top - floor(((double)m + log(fmin(c.min_p, 1.0)) / c.inv_t) * bins.inv_width);
+        bin_m = b < (double)kBins ? (unsigned int)fmax(b, 0.0) : kBins;
+    }
+    const unsigned int last = min(bin_p, bin_m);
+    if (last < kBins) {
+        if (!list_bin<W>(row_, bins, last, s, &count)) return false;
+        if (bin_m == last) {
+            // (whole numbers: their sum does not depend on the order in which the list was filled)
+            unsigned long long units = 0;
+            for (unsigned int i = tid; i < count; i += 64 * W) {
+                const double w = exp(-logit_depth(m, key_value(word_key(s.words[i])), c.inv_t));
+                if (w >= c.min_p) units += (unsigned long long)(w * kOne + 0.5);
+            }
+            units = block_reduce<W>(units, SumOp{}, s.search.sum[0]);
+            __syncthreads();
+            mass = fmin(mass, fmax((last ? s.sums[last - 1u] : 0.0) + (double)units * (1.0 / kOne), 1.0));
+        }
+        if (bin_p == last) {
+            if (count == 0) return false;
+            locate<W>(bins, last, count, most, false, m, c.inv_t, s);
+            mass = fmin(mass, s.part[0]);
+            __syncthreads();
+        }
+    }
+    // the choice
+    const bool end = !(c.u < 1.f);
+    const double drawn = end ? mass : c.u > 0.f ? (double)c.u * mass : 0.0;
+    const unsigned int bin = find_bin<W>(s, [&](double v) { return end ? v >= drawn : v > drawn; });
+    if (!list_bin<W>(row_, bins, bin, s, &count) || count == 0) return false;
+    locate<W>(bins, bin, count, drawn, !end, m, c.inv_t, s);
+    if (tid == 0)
+        put_choice(p, row, (int)word_index(s.word),
+                   (float)(-logit_depth(m, key_value(word_key(s.word)), c.inv_t) - log(mass)));
     return true;
 }
 
@@ -693,7 +812,7 @@ __device__ void choose_row(const Row& held, const ChooseArgs& p, unsigned long l
             const float t = top_threshold<W, SLOTS>(slot, m, c.k, s);
             const unsigned int count = gather_words<W>(held, s, [&](float x) { return x >= t; });
             if (count <= kList) {
-                sort_words<W>(s.words, count);
+                sort_words<W>(s, count);
                 if (threadIdx.x < 64) choose_from_list(p, row, c, s.words, count, m, s.sums);
                 done = true;
             }
@@ -801,7 +920,7 @@ __device__ void top_row(const Row& held, const TopArgs& p, unsigned long long ro
     }
     if (m > -INFINITY) {
         if (count > kList) count = top_by_search<W, T>(x, p.x.n, p.k, m, s);
-        sort_words<W>(s.words, count);
+        sort_words<W>(s, count);
     }
     put_top<W, T>(p, row, s.words, min(count, p.k));
 }
@@ -985,19 +1104,39 @@ __global__ __launch_bounds__(64 * W, EU) void top_piece_kernel(TopArgs p, Pieces
 }
 
 // The candidates of a row's pieces (up to 64) as a sorted list in LDS of which the first k are the row's; returns its length, or
-// more than kList if they do not fit.  m: the row's maximum.
+// more than kList if they do not fit.  m: the row's maximum.  A wavefront takes every W-th piece, and 64 candidates to a
+// register as long as there are some: one trip to memory, then three passes over registers; more are read again.
 template <int W>
 __device__ unsigned int join_words(const PieceHead* heads, const unsigned long long* words, unsigned int pieces, float m,
                                    unsigned int k, ChooseShared<W>& s) {
-    const unsigned int tid = threadIdx.x, lane = tid & 63u;
+    constexpr int kHeld = 8;
+    const unsigned int tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const unsigned int mine = lane < pieces ? heads[lane].taken : 0u;
     if (__ballot(mine > kList)) return kList + 1u;
     const unsigned int total = wave_reduce(mine, SumOp{});
+    const Global<unsigned long long>* in = global_in<unsigned long long>(words);
+    unsigned long long held[kHeld];
+    unsigned int q = wave, off = 0, held_now = 0;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        held[j] = 0;
+        while (q < pieces && off >= __builtin_amdgcn_readlane((int)mine, (int)q)) {
+            q += W;
+            off = 0;
+        }
+        if (q < pieces) {
+            if (off + lane < (unsigned int)__builtin_amdgcn_readlane((int)mine, (int)q)) held[j] = in[(size_t)q * kList + off + lane];
+            off += 64u;
+            held_now = j + 1;
+        }
+    }
     auto each_word = [&](auto f) {
-#pragma unroll 1
-        for (unsigned int q = 0; q < pieces; ++q) {
-            const unsigned int n = __shfl(mine, (int)q, 64);
-            for (unsigned int i = tid; i < n; i += 64 * W) f(global_in<unsigned long long>(words)[(size_t)q * kList + i]);
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            if (j < (int)held_now && held[j]) f(held[j]);
+        for (unsigned int r = q, at = off; r < pieces; r += W, at = 0) {
+            const unsigned int n = __builtin_amdgcn_readlane((int)mine, (int)r);
+            for (unsigned int i = at + lane; i < n; i += 64u) f(in[(size_t)r * kList + i]);
         }
     };
     float t = -3.402823466e38f;
@@ -1018,7 +1157,7 @@ __device__ unsigned int join_words(const PieceHead* heads, const unsigned long l
     __syncthreads();
     const unsigned int taken = s.taken;
     __syncthreads();
-    if (taken <= kList) sort_words<W>(s.words, taken);
+    if (taken <= kList) sort_words<W>(s, taken);
     return taken;
 }
 
@@ -1046,22 +1185,35 @@ __global__ __launch_bounds__(64 * W, 4) void choose_join_kernel(ChooseArgs p, Pi
         } else {
             const Bins bins(m, choice.inv_t);
             unsigned long long sum[kBins / (64 * W)] = {};
+            // bins between the row's first and each piece's, a lane for each
+            const double down = lane < c.count && heads[lane].m > -INFINITY ? bins.top - heads[lane].top : (double)kBins;
+            const unsigned int from = down < (double)kBins ? (unsigned int)down : kBins;
+            constexpr unsigned int kPer = kBins / (64 * W), kAhead = 8;
 #pragma unroll 1
-            for (unsigned int q = 0; q < c.count; ++q) {
-                const double down = bins.top - heads[q].top;   // bins between the row's first and the piece's
-                if (heads[q].m == -INFINITY || !(down < (double)kBins)) continue;
-                const unsigned int d = (unsigned int)down;
+            for (unsigned int q0 = 0; q0 < c.count; q0 += kAhead) {
+                unsigned long long piece[kAhead][kPer];
 #pragma unroll
-                for (unsigned int j = 0; j < kBins / (64 * W); ++j) {
-                    const unsigned int b = j * 64 * W + tid;
-                    if (b >= d) sum[j] += global_in<unsigned long long>(words)[(size_t)q * kBins + b - d];
+                for (unsigned int i = 0; i < kAhead; ++i) {
+                    // (pieces past the last one are that one again, and not added)
+                    const unsigned int q = min(q0 + i, c.count - 1u), d = __builtin_amdgcn_readlane((int)from, (int)q);
+#pragma unroll
+                    for (unsigned int j = 0; j < kPer; ++j) {
+                        const unsigned int bin = j * 64 * W + tid;
+                        const bool in = q0 + i < c.count && bin >= d;
+                        piece[i][j] = global_in<unsigned long long>(words)[(size_t)q * kBins + (in ? bin - d : 0u)];
+                        piece[i][j] = in ? piece[i][j] : 0ull;
+                    }
                 }
+#pragma unroll
+                for (unsigned int i = 0; i < kAhead; ++i)
+#pragma unroll
+                    for (unsigned int j = 0; j < kPer; ++j) sum[j] += piece[i][j];
             }
 #pragma unroll
             for (unsigned int j = 0; j < kBins / (64 * W); ++j) s.hist[j * 64 * W + tid] = sum[j];
             __syncthreads();
             sum_bins<W>(bins, m, s);
-            done = choose_from_bins<W>(ReadRow<W, T>(global_in<T>(p.x.data) + row * p.x.stride, 0, p.x.n), p, row, choice, bins, m, s);
+            done = choose_from_bins<W>(BatchRow<W, 8, T>(global_in<T>(p.x.data) + row * p.x.stride, 0, p.x.n), p, row, choice, bins, m, s);
         }
     }
     if (!done) {
@@ -1087,7 +1239,7 @@ __global__ __launch_bounds__(64 * W, 4) void top_join_kernel(TopArgs p, Pieces c
         count = join_words<W>(heads, ws.words + row * c.count * kList, c.count, m, p.k, s);
         if (count > kList) {
             count = top_by_search<W, T>(global_in<T>(p.x.data) + row * p.x.stride, p.x.n, p.k, m, s);
-            sort_words<W>(s.words, count);
+            sort_words<W>(s, count);
         }
     }
     put_top<W, T>(p, row, s.words, min(count, p.k));
@@ -1099,9 +1251,9 @@ template <typename T>
 Pieces pieces_of(unsigned long long rows, unsigned int n) {
     const unsigned int held = HeldRow<8, 8, T>::kMost;
     if (n <= held && (rows > 128u || n <= 8192u)) return Pieces{1u, n};
-    // pieces as long as a workgroup holds; shorter ones down to 4096 while there are fewer than 512
+    // pieces as long as a workgroup holds; shorter ones down to 8192 while there are fewer than 512
     unsigned int count = (n + held - 1u) / held;
-    const unsigned int fill = (unsigned int)((512u + rows - 1u) / rows), most = n / 4096u;
+    const unsigned int fill = (unsigned int)((512u + rows - 1u) / rows), most = n / 8192u;
     if (count < fill) count = fill < most ? fill : most > count ? most : count;
     if (count > 64u) count = 64u;
     const unsigned int length = (n / count + 63u) / 64u * 64u;
@@ -1150,7 +1302,7 @@ hipError_t launch_choose(const rp_rows* r, ChooseArgs a, void* workspace, hipStr
     for (unsigned long long at = 0; at < rows; at += step) {
         const unsigned int part = (unsigned int)(rows - at < step ? rows - at : step);
         choose_piece_kernel<8, 8, 4, T><<<dim3(c.count, part), 512, 0, st>>>(a, c, ws);
-        choose_join_kernel<8, T><<<part, 512, 0, st>>>(a, c, ws);
+        choose_join_kernel<16, T><<<part, 1024, 0, st>>>(a, c, ws);
         a.x.data += part * a.x.stride * sizeof(T);
         a.u += part;
         a.index += part;
@@ -1181,7 +1333,7 @@ hipError_t launch_top(const rp_rows* r, TopArgs a, void* workspace, hipStream_t 
     for (unsigned long long at = 0; at < rows; at += step) {
         const unsigned int part = (unsigned int)(rows - at < step ? rows - at : step);
         top_piece_kernel<8, 8, 4, T><<<dim3(c.count, part), 512, 0, st>>>(a, c, ws);
-        top_join_kernel<8, T><<<part, 512, 0, st>>>(a, c, ws);
+        top_join_kernel<16, T><<<part, 1024, 0, st>>>(a, c, ws);
         a.x.data += part * a.x.stride * sizeof(T);
         a.values += (size_t)part * a.k * sizeof(T);
         a.index += (size_t)part * a.k;

@@ -146,6 +146,21 @@ struct ReadRow {
     }
 };
 
+// The same, NV loads a thread at a time, all under way before the first is used: for passes whose loop the compiler does not
+// unroll.
+template <int W, int NV, typename T>
+struct BatchRow {
+    const Global<T>* x;
+    unsigned int begin, end;
+    __device__ __forceinline__ BatchRow(const Global<T>* x_, unsigned int begin_, unsigned int end_) : x(x_), begin(begin_), end(end_) {}
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        constexpr unsigned int kMost = HeldRow<W, NV, T>::kMost;
+#pragma unroll 1
+        for (unsigned int at = begin; at < end; at += kMost) HeldRow<W, NV, T>(x, at, min(at + kMost, end)).each(f);
+    }
+};
+
 // Unsigned integers in the order of the floats.
 __device__ __forceinline__ unsigned int order_key(float x) {
     const unsigned int b = __float_as_uint(x);

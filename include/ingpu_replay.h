@@ -423,6 +423,27 @@ rp_status rp_distill_loss(const rp_rows* logits, const rp_teacher* teacher, floa
 rp_status rp_distill_grad(const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad,
                           uint64_t grad_stride, void* workspace, size_t bytes, void* hip_stream);
 
+/*
+ * The operators on a trainer's own network.
+ */
+
+/* Bytes of device workspace train_act needs for `rows` (1 .. 2^20) states (0 if invalid). */
+size_t train_act_workspace_bytes(const train_config* cfg, uint32_t rows);
+
+/* Act: Q(s, .) of `rows` states (device, [rows*D] in the replay's state type) with the trained network's fp32 weights (in
+ * mixed precision too), then rp_choose_actions on them: temperature is that of Boltzmann exploration, 0 the greedy policy.
+ * action[rows], logp[rows] (may be NULL) and q[rows*A] (may be NULL: the Q-values) are device memory.  Neither trainer
+ * nor replay change, and train_get_last still reports the last step. */
+rp_status train_act(trainer_t* tr, uint32_t rows, const void* s, const rp_choice* how, const float* u, int32_t* action,
+                    float* logp, float* q, void* workspace, size_t bytes, void* hip_stream);
+
+/* One train step on the trainer's `batch` states s (device, [B*D] in the replay's state type) that learns from a teacher's top
+ * actions instead of rewards: loss and gradient are rp_distill_grad's on Q(s, .), their mean over the batch, weight included,
+ * is what is descended; optimizer, target network and step counters go on as in train_step_batch.  For trainers
+ * created with RP_TRAIN_LAYERED (else RP_EINVAL).  train_get_last reports the step's Q(s, .) and loss; its other fields are
+ * those of the TD step before. */
+rp_status train_distill_batch(trainer_t* tr, const void* s, const rp_teacher* teacher, void* hip_stream);
+
 /* Message for the last failure on this thread ("" if none). */
 const char* rp_last_error(void);
 /* Library version string. */

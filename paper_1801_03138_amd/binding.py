@@ -102,6 +102,9 @@ SYMBOLS = {
     "train_kernels_per_step": (_int, [_vp, _vp]),
     "train_set_handoff_wait": (_int, [_vp, _u64, _int]),
     "train_get_target_source": (_int, [_vp, _vp]),
+    "train_act_workspace_bytes": (C.c_size_t, [_vp, _u32]),
+    "train_act": (_int, [_vp, _u32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "train_distill_batch": (_int, [_vp, _vp, _vp, _vp]),
     "rp_choose_workspace_bytes": (C.c_size_t, [_vp]),
     "rp_choose_actions": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
     "rp_top_workspace_bytes": (C.c_size_t, [_vp, _u32]),
@@ -410,6 +413,32 @@ class Trainer:
         return _check(lib().train_step_batch(self._h, _dev(s), _dev(s_next), _dev(a), _dev(r),
                                              _dev(term), _stream_ptr(stream)))
 
+    def act(self, s, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, q=None, out=None, stream=None):
+        """One action per state (CUDA tensor [rows, D] of the replay's state type): Q-values of the trained network, then
+        choose_actions on them.  Returns (action int32[rows], logp float32[rows]); `q` (float32 [rows, actions])
+        receives the Q-values if given."""
+        rc, dev, rows = self.replay.cfg, self.replay.device, u.numel()
+        check_device_array(s, _TORCH_STATE[rc.state_dtype], rows * rc.state_dim, dev, "act: s")
+        if q is not None:
+            check_device_array(q, (torch.float32,), rows * self.cfg.num_actions, dev, "act: q")
+        with _On(s.device, stream):
+            how, u, out = _choice("act", rows, s.device, u, temperature, top_k, top_p, min_p, out)
+            nbytes = int(lib().train_act_workspace_bytes(C.byref(self.cfg), rows))
+            ws = _alloc_bytes(nbytes, s.device)
+            _check(lib().train_act(self._h, rows, _dev(s), C.byref(how), _dev(u), _dev(out[0]), _dev(out[1]), _dev(q),
+                                   _dev(ws), nbytes, _stream_ptr(stream)))
+        return out
+
+    def distill_batch(self, s, teacher, index, weight=None, teacher_lse=None, student_temperature=1.0,
+                      teacher_temperature=1.0, stream=None):
+        """One train step on `batch` states (as sample_gather returns them) that learns from a teacher's top actions, as
+        top_actions returns them, instead of rewards; the trainer must be a layered one."""
+        rc, dev = self.replay.cfg, self.replay.device
+        check_device_array(s, _TORCH_STATE[rc.state_dtype], self.cfg.batch * rc.state_dim, dev, "distill_batch: s")
+        t = _teacher(self.cfg.batch, s.device, teacher, index, weight, teacher_lse, student_temperature,
+                     teacher_temperature, "distill_batch")
+        return _check(lib().train_distill_batch(self._h, _dev(s), C.byref(t), _stream_ptr(stream)))
+
     def params(self):
         p = np.empty(self.n_params, np.float32)
         _check(lib().train_get_params(self._h, _host(p)))
@@ -573,31 +602,37 @@ def _workspace(nbytes, workspace, device, what):
     return (workspace, None, 0) if workspace is None else (workspace, workspace.data_ptr(), workspace.numel())
 
 
+def _choice(what, rows, dev, u, temperature, top_k, top_p, min_p, out):
+    """Checked settings, random numbers and outputs of a choice: (Choice, u, (index, logp)).  The settings' arrays are the
+    caller's to keep alive."""
+    check_device_array(u, (torch.float32,), rows, dev, what + ": u")
+    t, t_row = check_setting(temperature, torch.float32, rows, dev, what + ": temperature")
+    k, k_row = check_setting(top_k, torch.int32, rows, dev, what + ": top_k")
+    p, p_row = check_setting(top_p, torch.float32, rows, dev, what + ": top_p")
+    m, m_row = check_setting(min_p, torch.float32, rows, dev, what + ": min_p")
+    if out is None:
+        out = (torch.empty(rows, dtype=torch.int32, device=dev), torch.empty(rows, dtype=torch.float32, device=dev))
+    else:
+        check_device_array(out[0], (torch.int32,), rows, dev, what + ": index")
+        if out[1] is not None:
+            check_device_array(out[1], (torch.float32,), rows, dev, what + ": logp")
+    return Choice(1.0 if t is None else t, 1.0 if p is None else p, 0.0 if m is None else m, 0 if k is None else k,
+                  _dev(t_row), _dev(p_row), _dev(m_row), _dev(k_row)), u, out
+
+
 def choose_actions(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, workspace=None, stream=None):
     """One action per row of logits (or Q-values) from the random numbers u[rows] in [0, 1): see
     rp_choose_actions.  Each setting is a number, or a device tensor with one per row (float32; top_k int32).
     Returns (index int32[rows], logp float32[rows]), in `out` if given."""
     check_rows(logits, "choose_actions: logits")
     rows, dev = logits.shape[0], logits.device
-    check_device_array(u, (torch.float32,), rows, dev, "choose_actions: u")
-    t, t_row = check_setting(temperature, torch.float32, rows, dev, "choose_actions: temperature")
-    k, k_row = check_setting(top_k, torch.int32, rows, dev, "choose_actions: top_k")
-    p, p_row = check_setting(top_p, torch.float32, rows, dev, "choose_actions: top_p")
-    m, m_row = check_setting(min_p, torch.float32, rows, dev, "choose_actions: min_p")
     with _On(dev, stream):
-        if out is None:
-            out = (torch.empty(rows, dtype=torch.int32, device=dev), torch.empty(rows, dtype=torch.float32, device=dev))
-        index, logp = out
-        check_device_array(index, (torch.int32,), rows, dev, "choose_actions: index")
-        if logp is not None:
-            check_device_array(logp, (torch.float32,), rows, dev, "choose_actions: logp")
+        how, u, out = _choice("choose_actions", rows, dev, u, temperature, top_k, top_p, min_p, out)
         x = _logit_rows(logits)
-        how = Choice(1.0 if t is None else t, 1.0 if p is None else p, 0.0 if m is None else m, 0 if k is None else k,
-                     _dev(t_row), _dev(p_row), _dev(m_row), _dev(k_row))
         hold, ws, nbytes = _workspace(lib().rp_choose_workspace_bytes(C.byref(x)), workspace, dev, "choose_actions")
-        _check(lib().rp_choose_actions(C.byref(x), C.byref(how), u.data_ptr(), index.data_ptr(), _dev(logp), ws, nbytes,
+        _check(lib().rp_choose_actions(C.byref(x), C.byref(how), u.data_ptr(), out[0].data_ptr(), _dev(out[1]), ws, nbytes,
                                        _stream_ptr(stream)))
-    return index, logp
+    return out
 
 
 def top_actions(logits, k, temperature=1.0, out=None, workspace=None, stream=None):
@@ -623,9 +658,7 @@ def top_actions(logits, k, temperature=1.0, out=None, workspace=None, stream=Non
     return values, index, lse
 
 
-def _teacher(logits, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, what):
-    check_rows(logits, what + ": logits")
-    rows, dev = logits.shape[0], logits.device
+def _teacher(rows, dev, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, what):
     if not isinstance(index, torch.Tensor) or index.dim() != 2 or index.shape[0] != rows:
         raise ValueError(f"{what}: index must be a rows x k tensor")
     k = index.shape[1]
@@ -635,16 +668,18 @@ def _teacher(logits, teacher, index, weight, teacher_lse, student_temperature, t
         check_device_array(teacher_lse, (torch.float32,), rows, dev, what + ": teacher_lse")
     if weight is not None:
         check_device_array(weight, (torch.float32,), rows, dev, what + ": weight")
-    return _logit_rows(logits), Teacher(teacher.data_ptr(), index.data_ptr(), _dev(teacher_lse), _dev(weight), k,
-                                        _LOGIT_DTYPE[teacher.dtype], teacher_temperature, student_temperature)
+    return Teacher(teacher.data_ptr(), index.data_ptr(), _dev(teacher_lse), _dev(weight), k, _LOGIT_DTYPE[teacher.dtype],
+                   teacher_temperature, student_temperature)
 
 
 def distill_loss(logits, teacher, index, weight=None, teacher_lse=None, student_temperature=1.0,
                  teacher_temperature=1.0, out=None, workspace=None, stream=None):
     """Loss of every row of the student's logits against a teacher's top logits [rows, k] and their actions, as
     top_actions returns them: see rp_distill_loss.  Returns float32[rows]."""
-    rows, dev = len(logits), logits.device
-    x, t = _teacher(logits, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_loss")
+    check_rows(logits, "distill_loss: logits")
+    rows, dev = logits.shape[0], logits.device
+    x = _logit_rows(logits)
+    t = _teacher(rows, dev, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_loss")
     with _On(dev, stream):
         hold, ws, nbytes = _workspace(lib().rp_distill_workspace_bytes(C.byref(x), t.k), workspace, dev, "distill_loss")
         out = torch.empty(rows, dtype=torch.float32, device=dev) if out is None else out
@@ -658,8 +693,10 @@ def distill_grad(logits, teacher, index, weight=None, teacher_lse=None, student_
     """distill_loss and its gradient with respect to the logits: see rp_distill_grad.  Returns (loss float32[rows],
     gradient [rows, n] in the logits' type); `out` = (loss, gradient), the gradient at any row stride, also
     the logits themselves."""
-    rows, dev = len(logits), logits.device
-    x, t = _teacher(logits, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_grad")
+    check_rows(logits, "distill_grad: logits")
+    rows, dev = logits.shape[0], logits.device
+    x = _logit_rows(logits)
+    t = _teacher(rows, dev, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_grad")
     with _On(dev, stream):
         hold, ws, nbytes = _workspace(lib().rp_distill_workspace_bytes(C.byref(x), t.k), workspace, dev, "distill_grad")
         if out is None:

@@ -12,6 +12,7 @@ struct DistillArgs {
     const float* weight;          // or null
     unsigned int k;
     double inv_tt, inv_ts;        // 1 / temperature of teacher, of student
+    double scale;                 // of the gradient
     float c2;                     // log2(e) / student's temperature
     float* loss;
     unsigned char* grad;
@@ -294,7 +295,7 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     if (bad) loss = NAN;
     if (lane == 0) {
         if (put_loss) p.loss[row] = empty ? 0.f : (float)(loss * (double)weight);
-        const double scale = (double)weight * p.inv_ts;
+        const double scale = (double)weight * p.scale * p.inv_ts;
         *out = RowScalars{m > -INFINITY ? m : 0.f, bad ? NAN : (float)(scale * outside / total), shift, q_scale, inside, scale,
                           1.0 / total, empty ? 1u : bad ? 2u : 0u};
     }
@@ -633,8 +634,10 @@ hipError_t launch_distill(const DistillArgs& a, bool gradient, void* ws, hipStre
     return gradient ? launch_rows<T, TT, false, true>(a, ws, st) : launch_rows<T, TT, false, false>(a, ws, st);
 }
 
-rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad,
-                  uint64_t grad_stride, bool gradient, void* workspace, size_t bytes, void* hip_stream) {
+}  // namespace
+
+rp_status distill_rows(const char* what, const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad,
+                       uint64_t grad_stride, bool gradient, double scale, void* workspace, size_t bytes, void* hip_stream) {
     const char* why = logit_rows_fault(logits);
     RP_REQUIRE(!why, "%s: %s", what, why);
     RP_REQUIRE(teacher, "%s: null teacher", what);
@@ -664,7 +667,7 @@ rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* tea
         return RP_ENOMEM;
     }
     const DistillArgs a{logit_rows(logits), static_cast<const unsigned char*>(teacher->value), teacher->index, teacher->lse,
-                        teacher->weight, teacher->k, 1.0 / teacher->temperature, 1.0 / teacher->student_temperature,
+                        teacher->weight, teacher->k, 1.0 / teacher->temperature, 1.0 / teacher->student_temperature, scale,
                         (float)(1.4426950408889634 / teacher->student_temperature), loss,
                         static_cast<unsigned char*>(grad), grad_stride};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -675,7 +678,6 @@ rp_status distill(const char* what, const rp_rows* logits, const rp_teacher* tea
     return RP_OK;
 }
 
-}  // namespace
 }  // namespace rp
 
 extern "C" {
@@ -692,12 +694,12 @@ size_t rp_distill_workspace_bytes(const rp_rows* logits, uint32_t k) {
 
 rp_status rp_distill_loss(const rp_rows* logits, const rp_teacher* teacher, float* loss, void* workspace, size_t bytes,
                           void* hip_stream) {
-    return rp::distill("rp_distill_loss", logits, teacher, loss, nullptr, 0, false, workspace, bytes, hip_stream);
+    return rp::distill_rows("rp_distill_loss", logits, teacher, loss, nullptr, 0, false, 1.0, workspace, bytes, hip_stream);
 }
 
 rp_status rp_distill_grad(const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad, uint64_t grad_stride,
                           void* workspace, size_t bytes, void* hip_stream) {
-    return rp::distill("rp_distill_grad", logits, teacher, loss, grad, grad_stride, true, workspace, bytes, hip_stream);
+    return rp::distill_rows("rp_distill_grad", logits, teacher, loss, grad, grad_stride, true, 1.0, workspace, bytes, hip_stream);
 }
 
 }  // extern "C"

@@ -250,4 +250,9 @@ inline LogitRows logit_rows(const rp_rows* r) {
     return LogitRows{static_cast<const unsigned char*>(r->data), r->rows, r->stride, r->n};
 }
 
+// rp_distill_loss (gradient false) and rp_distill_grad, the gradient times `scale` as well; `what` names the entry point in
+// messages.
+rp_status distill_rows(const char* what, const rp_rows* logits, const rp_teacher* teacher, float* loss, void* grad,
+                       uint64_t grad_stride, bool gradient, double scale, void* workspace, size_t bytes, void* hip_stream);
+
 }  // namespace rp

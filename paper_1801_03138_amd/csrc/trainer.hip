@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "common.hpp"
+#include "logits.hpp"
 #include "replay_kernels.hpp"
 #include "trainer.hpp"
 
@@ -238,6 +239,27 @@ __global__ __launch_bounds__(kThreads) void load_batch_kernel(
         rew[e] = r[e];
         trm[e] = term[e] ? 1 : 0;
         idx[e] = (unsigned int)e;
+    }
+}
+
+// Given states into the first half of X, for a step that needs nothing else of a batch; thread 0 of block 0 also advances
+// Adam's step count and its bias corrections, as td_loss_kernel does for the other steps.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void load_states_kernel(unsigned int B, unsigned int D, unsigned int Dp,
+                                                               const E* __restrict__ s, E* __restrict__ X,
+                                                               TrainCounters* __restrict__ ctr, float beta1, float beta2) {
+    const size_t e = (size_t)blockIdx.x * kThreads + threadIdx.x;
+    if (e == 0) {
+        const double pw1 = ctr->pw1 * (double)beta1, pw2 = ctr->pw2 * (double)beta2;
+        ctr->adam_t = ctr->adam_t + 1;
+        ctr->pw1 = pw1;
+        ctr->pw2 = pw2;
+        ctr->c1 = (float)(1.0 - pw1);
+        ctr->c2 = (float)(1.0 - pw2);
+    }
+    if (e < (size_t)B * D) {
+        const unsigned int i = (unsigned int)(e / D), c = (unsigned int)(e - (size_t)i * D);
+        X[(size_t)i * Dp + c] = s[e];
     }
 }
 
@@ -484,6 +506,40 @@ void gemm(hipStream_t st, int M, int N, int K, const void* A, int lda, const voi
                        static_cast<TC*>(C), ldc, bias, static_cast<const TC*>(mask), ldmask);
 }
 
+// The end of a layered step: from dZ2 the gradients of the hidden layers, and the update of all of them.
+template <typename E>
+hipError_t enqueue_hidden_and_update(trainer* t, hipStream_t st, unsigned int* count) {
+    const int B = (int)t->B, H = (int)t->H, G = (int)t->Hb, Dp = (int)t->Dp;
+    const unsigned char* wsrc = t->cfg.param_dtype == RP_BF16 ? reinterpret_cast<const unsigned char*>(t->wb)
+                                                              : reinterpret_cast<const unsigned char*>(t->w);
+    const void* W2 = wsrc + t->oW2 * t->elem;
+    unsigned int n = 0;
+    // second hidden layer
+    gemm<E, E, float, true, false, EPI_NONE>(st, H, G, B, t->H1, H, t->dZ2, G, t->g + t->oW2, G,
+                                             nullptr, nullptr, 0); ++n;
+    hipLaunchKernelGGL(colsum_kernel<E>, dim3((G + kThreads - 1) / kThreads), dim3(kThreads), 0, st,
+                       B, G, static_cast<const E*>(t->dZ2), G, t->g + t->ob2); ++n;
+    gemm<E, E, E, false, true, EPI_MASK>(st, B, H, G, t->dZ2, G, W2, G, t->dZ1, H, nullptr, t->H1,
+                                         H); ++n;
+    // first hidden layer
+    gemm<E, E, float, true, false, EPI_NONE>(st, Dp, H, B, t->X, Dp, t->dZ1, H, t->g + t->oW1, H,
+                                             nullptr, nullptr, 0); ++n;
+    hipLaunchKernelGGL(colsum_kernel<E>, dim3((H + kThreads - 1) / kThreads), dim3(kThreads), 0, st,
+                       B, H, static_cast<const E*>(t->dZ1), H, t->g + t->ob1); ++n;
+    // update
+    // (with the dueling head the output layer's update belongs to the head kernel)
+    const unsigned int n_opt = (unsigned int)(t->dueling ? t->oW3 : t->n_padded);
+    hipLaunchKernelGGL(optimizer_kernel, dim3((n_opt + kThreads - 1) / kThreads),
+                       dim3(kThreads), 0, st, n_opt, t->w, t->g, t->m, t->v,
+                       t->wb, t->cfg.opt, t->cfg.lr, t->cfg.beta1, t->cfg.beta2, t->cfg.eps, t->ctr,
+                       t->lossi, t->B, t->wt, t->wbt, t->cfg.target_sync); ++n;
+    unsigned int nh = 0;
+    hipError_t e = enqueue_head_update(t, st, &nh);
+    if (e != hipSuccess) return e;
+    *count = n + nh;
+    return hipGetLastError();
+}
+
 // Enqueue every kernel of one executed train step (after the append).  E is the element
 // type of activations and of the matrices the products read.
 template <typename E>
@@ -554,27 +610,8 @@ hipError_t enqueue_step(trainer* t, hipStream_t st, unsigned int* count, bool sa
                        dim3(kThreads), 0, st, t->B, t->Hb, A, t->Ap, t->dQ, t->act,
                        static_cast<const E*>(W3), static_cast<const E*>(t->H2),
                        static_cast<E*>(t->dZ2)); ++n;
-    // second hidden layer
-    gemm<E, E, float, true, false, EPI_NONE>(st, H, G, B, t->H1, H, t->dZ2, G, t->g + t->oW2, G,
-                                             nullptr, nullptr, 0); ++n;
-    hipLaunchKernelGGL(colsum_kernel<E>, dim3((G + kThreads - 1) / kThreads), dim3(kThreads), 0, st,
-                       B, G, static_cast<const E*>(t->dZ2), G, t->g + t->ob2); ++n;
-    gemm<E, E, E, false, true, EPI_MASK>(st, B, H, G, t->dZ2, G, W2, G, t->dZ1, H, nullptr, t->H1,
-                                         H); ++n;
-    // first hidden layer
-    gemm<E, E, float, true, false, EPI_NONE>(st, Dp, H, B, t->X, Dp, t->dZ1, H, t->g + t->oW1, H,
-                                             nullptr, nullptr, 0); ++n;
-    hipLaunchKernelGGL(colsum_kernel<E>, dim3((H + kThreads - 1) / kThreads), dim3(kThreads), 0, st,
-                       B, H, static_cast<const E*>(t->dZ1), H, t->g + t->ob1); ++n;
-    // update
-    // (with the dueling head the output layer's update belongs to the head kernel)
-    const unsigned int n_opt = (unsigned int)(t->dueling ? t->oW3 : t->n_padded);
-    hipLaunchKernelGGL(optimizer_kernel, dim3((n_opt + kThreads - 1) / kThreads),
-                       dim3(kThreads), 0, st, n_opt, t->w, t->g, t->m, t->v,
-                       t->wb, t->cfg.opt, t->cfg.lr, t->cfg.beta1, t->cfg.beta2, t->cfg.eps, t->ctr,
-                       t->lossi, t->B, t->wt, t->wbt, t->cfg.target_sync); ++n;
     unsigned int nh = 0;
-    e = enqueue_head_update(t, st, &nh);
+    e = enqueue_hidden_and_update<E>(t, st, &nh);
     if (e != hipSuccess) return e;
     if (count) *count = n + nh;
     return hipGetLastError();
@@ -634,6 +671,59 @@ hipError_t enqueue_append_and_step(trainer* t, const Payload& src, hipStream_t s
                                                    : enqueue_step<float>(t, st, &k, true);
     if (count) *count = n + k;
     return e;
+}
+
+// A layered step whose loss is the distillation from a teacher's top logits instead of the TD error: forward on the
+// given states alone, the loss's gradient with respect to every Q-value, backward, update.
+template <typename E>
+hipError_t enqueue_distill_step(trainer* t, const E* states, const rp_teacher* teacher, hipStream_t st, rp_status* refused) {
+    const int B = (int)t->B, H = (int)t->H, G = (int)t->Hb, Dp = (int)t->Dp, Ap = (int)t->Ap;
+    const unsigned int A = t->cfg.num_actions, D = t->cfg.state_dim;
+    const unsigned char* wsrc = t->cfg.param_dtype == RP_BF16 ? reinterpret_cast<const unsigned char*>(t->wb)
+                                                              : reinterpret_cast<const unsigned char*>(t->w);
+    const void* W3 = wsrc + t->oW3 * t->elem;
+    hipLaunchKernelGGL(load_states_kernel<E>, dim3((unsigned int)(((size_t)B * D + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                       st, t->B, D, t->Dp, states, static_cast<E*>(t->X), t->ctr, t->cfg.beta1, t->cfg.beta2);
+    gemm<E, E, E, false, false, EPI_BIAS_RELU>(st, B, H, Dp, t->X, Dp, wsrc + t->oW1 * t->elem, H, t->H1, H, t->w + t->ob1,
+                                               nullptr, 0);
+    gemm<E, E, E, false, false, EPI_BIAS_RELU>(st, B, G, H, t->H1, H, wsrc + t->oW2 * t->elem, G, t->H2, G, t->w + t->ob2,
+                                               nullptr, 0);
+    gemm<E, E, float, false, false, EPI_BIAS>(st, B, Ap, G, t->H2, G, W3, Ap, t->Q, Ap, t->w + t->ob3, nullptr, 0);
+    // (the columns past the last action stay zero, as the TD step leaves them)
+    const rp_rows q{t->Q, (uint64_t)B, (uint64_t)Ap, A, RP_F32};
+    *refused = distill_rows("train_distill_batch", &q, teacher, t->lossi, t->dQ, (uint64_t)Ap, true, 1.0 / B, nullptr, 0, st);
+    if (*refused != RP_OK) return hipSuccess;
+    gemm<E, float, float, true, false, EPI_NONE>(st, G, Ap, B, t->H2, G, t->dQ, Ap, t->g + t->oW3, Ap, nullptr, nullptr, 0);
+    hipLaunchKernelGGL(colsum_kernel<float>, dim3((Ap + kThreads - 1) / kThreads), dim3(kThreads), 0, st, B, Ap, t->dQ, Ap,
+                       t->g + t->ob3);
+    gemm<float, E, E, false, true, EPI_MASK>(st, B, G, Ap, t->dQ, Ap, W3, Ap, t->dZ2, G, nullptr, t->H2, G);
+    unsigned int n = 0;
+    return enqueue_hidden_and_update<E>(t, st, &n);
+}
+
+// Q(s, .) of any number of states with the trained network's fp32 weights: three plain products.
+template <typename E>
+hipError_t enqueue_q_values(const trainer* t, unsigned int rows, const void* states, float* H1, float* H2, float* Q,
+                            hipStream_t st) {
+    const int M = (int)rows, H = (int)t->H, G = (int)t->Hb, D = (int)t->cfg.state_dim, A = (int)t->cfg.num_actions;
+    gemm<E, float, float, false, false, EPI_BIAS_RELU>(st, M, H, D, states, D, t->w + t->oW1, H, H1, H, t->w + t->ob1, nullptr, 0);
+    gemm<float, float, float, false, false, EPI_BIAS_RELU>(st, M, G, H, H1, H, t->w + t->oW2, G, H2, G, t->w + t->ob2, nullptr, 0);
+    gemm<float, float, float, false, false, EPI_BIAS>(st, M, A, G, H2, G, t->w + t->oW3, (int)t->Ap, Q, A, t->w + t->ob3, nullptr, 0);
+    return hipGetLastError();
+}
+
+struct ActLayout {
+    size_t h1, h2, q, total;
+};
+bool act_layout(const train_config* cfg, uint32_t rows, ActLayout* L) {
+    WsLayout ws;
+    if (!ws_layout(cfg, &ws) || rows == 0 || rows > (1u << 20)) return false;
+    const size_t H = cfg->hidden, G = cfg->hidden2 ? cfg->hidden2 : cfg->hidden;
+    L->h1 = 0;
+    L->h2 = align_up(L->h1 + rows * H * 4, 256);
+    L->q = align_up(L->h2 + rows * G * 4, 256);
+    L->total = align_up(L->q + (size_t)rows * cfg->num_actions * 4, 256);
+    return true;
 }
 
 // Enqueue one step on a caller-provided batch (device arrays): no append, no sampling.
@@ -1126,6 +1216,51 @@ rp_status train_step_batch(trainer_t* t, const void* s, const void* s_next, cons
     t->host_step += 1;
     t->host_adam_t += 1;
     return RP_OK;
+}
+
+rp_status train_distill_batch(trainer_t* t, const void* s, const rp_teacher* teacher, void* hip_stream) {
+    RP_REQUIRE(t && s && teacher, "train_distill_batch: null argument");
+    RP_REQUIRE(!t->fused && !t->wide && !t->mid, "train_distill_batch: the trainer was not created with RP_TRAIN_LAYERED");
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    // (a teacher that the loss refuses is refused before anything of the step runs)
+    const rp_rows none{nullptr, 0, 0, t->cfg.num_actions, RP_F32};
+    rp_status refused = rp::distill_rows("train_distill_batch", &none, teacher, nullptr, nullptr, 0, true, 1.0, nullptr, 0, st);
+    if (refused != RP_OK) return refused;
+    RP_REQUIRE(teacher->value && teacher->index, "train_distill_batch: null array");
+    RP_CHECK_HIP(t->cfg.param_dtype == RP_BF16
+                     ? rp::enqueue_distill_step<bf16_t>(t, static_cast<const bf16_t*>(s), teacher, st, &refused)
+                     : rp::enqueue_distill_step<float>(t, static_cast<const float*>(s), teacher, st, &refused));
+    if (refused != RP_OK) return refused;
+    t->host_step += 1;
+    t->host_adam_t += 1;
+    return RP_OK;
+}
+
+size_t train_act_workspace_bytes(const train_config* cfg, uint32_t rows) {
+    rp::ActLayout L;
+    return rp::act_layout(cfg, rows, &L) ? L.total : 0;
+}
+
+rp_status train_act(trainer_t* t, uint32_t rows, const void* s, const rp_choice* how, const float* u, int32_t* action,
+                    float* logp, float* q, void* workspace, size_t bytes, void* hip_stream) {
+    RP_REQUIRE(t, "train_act: null handle");
+    rp::ActLayout L;
+    RP_REQUIRE(rp::act_layout(&t->cfg, rows, &L), "train_act: 1 to 2^20 states");
+    RP_REQUIRE(s && how && u && action, "train_act: null argument");
+    if (const char* fault = rp::workspace_fault(workspace, bytes, L.total)) {
+        rp::set_error("train_act: %s (%zu bytes given, %zu needed)", fault, bytes, L.total);
+        return RP_ENOMEM;
+    }
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    float* h1 = reinterpret_cast<float*>(ws + L.h1);
+    float* h2 = reinterpret_cast<float*>(ws + L.h2);
+    if (!q) q = reinterpret_cast<float*>(ws + L.q);
+    RP_CHECK_HIP(t->cfg.param_dtype == RP_BF16 ? rp::enqueue_q_values<bf16_t>(t, rows, s, h1, h2, q, st)
+                                               : rp::enqueue_q_values<float>(t, rows, s, h1, h2, q, st));
+    // (at most 4096 actions: the choice needs no workspace)
+    const rp_rows x{q, rows, t->cfg.num_actions, t->cfg.num_actions, RP_F32};
+    return rp_choose_actions(&x, how, u, action, logp, nullptr, 0, hip_stream);
 }
 
 rp_status train_steps(trainer_t* t, uint64_t count, const void* s, const void* s_next,

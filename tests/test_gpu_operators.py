@@ -445,3 +445,184 @@ def test_a_table_beyond_4_gib(B):
     loss, grad = B.distill_grad(x, value, top, teacher_lse=lse, student_temperature=2.0)
     a, b = B.distill_grad(few, value[last].clone(), top[last].clone(), teacher_lse=lse[last].clone(), student_temperature=2.0)
     assert torch.equal(loss[last], a) and torch.equal(grad[last], b)
+
+
+# ------------------------------------------------------------------------- on a trainer's own network
+def trainer(B, dtype="f32", D=27, H=64, G=0, A=30, batch=64, dueling=False, layered=False, opt=None, seed=3, **kw):
+    from paper_1801_03138_amd import synth
+    st = B.RP_F32 if dtype == "f32" else B.RP_BF16
+    ring = B.Replay(512, D, st, seed=seed)
+    rows = synth.experiences(512, D, A, 0.02, seed=seed, state_dtype=dtype)
+    ring.append(rows["s"], rows["s_next"], rows["a"], rows["r"], rows["term"])
+    p = synth.init_params(D, H, A + (1 if dueling else 0), seed, hidden2=G or None)
+    return B.Trainer(ring, H, A, batch, param_dtype=st, opt=B.RP_SGD if opt is None else opt, lr=1e-2, appends_per_step=0,
+                     dueling=dueling, layered=layered, hidden2=G, init_params=p, **kw)
+
+
+def network(params, D, H, G, A, dueling, X):
+    """Q(s, .) with 64-bit torch tensors; params in the trainer's order, requiring gradients."""
+    G, O = G or H, A + (1 if dueling else 0)
+    at, parts = 0, []
+    for shape in ((D, H), (H,), (H, G), (G,), (G, O), (O,)):
+        n = int(np.prod(shape))
+        parts.append(params[at:at + n].view(shape))
+        at += n
+    W1, b1, W2, b2, W3, b3 = parts
+    h = torch.relu(torch.relu(X @ W1 + b1) @ W2 + b2)
+    if not dueling:
+        return h @ W3 + b3
+    v = h[:, :G // 2] @ W3[:G // 2, :1] + b3[:1]
+    a = h[:, G // 2:] @ W3[G // 2:, 1:] + b3[1:]
+    return v + a - a.mean(dim=1, keepdim=True)
+
+
+@pytest.mark.parametrize("dtype,H,G,A,dueling,layered", [
+    ("f32", 64, 0, 30, False, False), ("f32", 128, 256, 30, True, False), ("f32", 320, 0, 100, False, False),
+    ("f32", 64, 0, 5, True, True), ("bf16", 128, 0, 30, False, False), ("bf16", 64, 0, 30, True, True)])
+def test_a_trainer_acts_with_its_network(B, dtype, H, G, A, dueling, layered):
+    """Q-values to the rounding of the products (contractions of up to 320 terms in 32 bits, three of them: 2^-24 a term
+    and product relative to the largest sum of magnitudes, here under 8 times the largest Q), choices as the
+    definition has them on those Q-values, and nothing of the trainer changed."""
+    tr = trainer(B, dtype, H=H, G=G, A=A, dueling=dueling, layered=layered, target_sync=3)
+    for _ in range(4):
+        tr.step()
+    p, last = tr.params(), tr.last()
+    rng = np.random.default_rng(0)
+    for rows in (1, 3, 64, 517):
+        s = torch.from_numpy(rng.normal(size=(rows, 27)).astype(np.float32)).to(DT[dtype]).cuda()
+        u = draw_u(rng, rows)
+        q = torch.empty((rows, A), device="cuda")
+        how = {"temperature": 0.5, "top_k": 4, "top_p": 0.9}
+        action, logp = tr.act(s, torch.from_numpy(u).cuda(), q=q, **how)
+        again, _ = tr.act(s, torch.from_numpy(u).cuda(), **how)
+        want = network(torch.from_numpy(p).double(), 27, H, G, A, dueling, s.double().cpu()).numpy()
+        got = q.double().cpu().numpy()
+        assert np.abs(got - want).max() <= 8 * 2.0 ** -24 * (27 + H + (G or H)) * np.abs(want).max()
+        check_choice(got, u, how, action, logp)
+        assert torch.equal(action, again)
+        best, _ = tr.act(s, torch.from_numpy(u).cuda(), temperature=0.0)
+        assert np.array_equal(best.cpu().numpy(), got.argmax(1))
+    assert np.array_equal(tr.params(), p)
+    now = tr.last()
+    assert all(np.array_equal(now[k], last[k]) for k in ("Q", "y", "delta", "idx")) and now["loss"] == last["loss"]
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("dtype,G,A,dueling", [("f32", 0, 30, False), ("f32", 128, 30, True), ("f32", 0, 300, False),
+                                               ("bf16", 0, 30, False)])
+def test_a_step_on_a_teachers_actions(B, dtype, G, A, dueling, rest):
+    """The step's gradient against automatic differentiation of the same loss in 64 bits, its update against that gradient.
+    Sums of up to D + H + G + B terms in 32 bits: 2^-24 a term, relative to sums of magnitudes of up to 4 times the largest
+    entry.  bf16: six roundings to 2^-8 on the way (states' and weights' are in the reference too), twice that for units
+    at the kink."""
+    D, H, batch, k = 27, 64, 64, 6
+    tr = trainer(B, dtype, G=G, A=A, dueling=dueling, layered=True)
+    rng = np.random.default_rng(A)
+    s = torch.from_numpy(rng.normal(size=(batch, D)).astype(np.float32)).to(DT[dtype]).cuda()
+    t = rng.normal(0, 1, (batch, A)).astype(np.float32)
+    index = np.argsort(-t, axis=1)[:, :k].astype(np.int32)
+    index[::7, -1] = -1
+    value = np.take_along_axis(t, np.maximum(index, 0), 1)
+    lse = np.array([ref.log_sum_exp(r, 0.5) for r in t], np.float32)
+    weight = rng.uniform(0.5, 1.5, batch).astype(np.float32)
+    weight[5] = 0.0
+    p0 = tr.params()
+    cuda = lambda v: torch.from_numpy(v).cuda()
+    tr.distill_batch(s, cuda(value), cuda(index), weight=cuda(weight), teacher_lse=cuda(lse) if rest else None,
+                     student_temperature=0.7, teacher_temperature=0.5)
+    # the reference
+    p = torch.from_numpy(p0)
+    p = (p.to(torch.bfloat16) if dtype == "bf16" else p).double().requires_grad_()
+    z = network(p, D, H, G, A, dueling, s.double().cpu()) / 0.7
+    log_p = torch.log_softmax(z, dim=1)
+    there = torch.from_numpy(index >= 0)
+    tt = torch.from_numpy(value).double() / 0.5
+    tt = torch.where(there, tt, -INF)
+    log_q = tt - torch.from_numpy(lse).double()[:, None] if rest else torch.log_softmax(tt, dim=1)
+    q = log_q.exp()
+    at = torch.from_numpy(np.maximum(index, 0)).long()
+    picked = torch.gather(log_p, 1, at)
+    loss = torch.where(there, q * (torch.where(there, log_q, 0.0) - picked), 0.0).sum(1)
+    if rest:
+        q_rest = 1 - q.sum(1)
+        p_rest = 1 - torch.where(there, picked.exp(), 0.0).sum(1)
+        loss = loss + q_rest * (q_rest.log() - p_rest.log())
+    loss = (loss * torch.from_numpy(weight).double()).mean()
+    loss.backward()
+    want, got = p.grad.numpy(), tr.grads()
+    tol = 4 * 2.0 ** -24 * (D + H + (G or H) + batch + A) if dtype == "f32" else 12 * 2.0 ** -8
+    assert np.abs(got - want).max() <= tol * np.abs(want).max()
+    last = tr.last()
+    # (32 bits: each row's loss to 2^-22 (log A + 4) of its size and the Q-values' error of before)
+    q_off = 8 * 2.0 ** -24 * (D + H + (G or H)) if dtype == "f32" else 6 * 2.0 ** -8
+    assert abs(last["loss"] - loss.item()) <= 2.0 ** -22 * (math.log(A) + 4) + 4 * q_off * np.abs(last["Q"]).max() / 0.7
+    step = np.float32(1e-2) * got
+    assert np.abs(tr.params() - (p0 - step)).max() <= 2.0 ** -23 * np.abs(p0).max()
+    assert tr.opt_state()[2:] == (1, 1)
+    # the trainer goes on: a TD step after it counts on
+    assert tr.step() == 0 and tr.opt_state()[2:] == (2, 2)
+
+
+def test_adam_on_a_teachers_actions_counts_its_steps(B):
+    """Two steps of Adam from its own definition on the gradients the trainer reports."""
+    tr = trainer(B, layered=True, opt=B.RP_ADAM)
+    s = torch.randn((64, 27), device="cuda")
+    value, index, lse = B.top_actions(torch.randn((64, 30), device="cuda"), 5)
+    m = v = 0.0
+    p = tr.params().astype(np.float64)
+    for t in (1, 2):
+        tr.distill_batch(s, value, index, teacher_lse=lse)
+        g = tr.grads().astype(np.float64)
+        m, v = 0.9 * m + 0.1 * g, 0.999 * v + 0.001 * g * g
+        step = 1e-2 * (m / (1 - 0.9 ** t)) / (np.sqrt(v / (1 - 0.999 ** t)) + 1e-8)
+        # (moments, corrections, root and quotient in 32 bits: under 16 roundings of the step, and 1 - 0.999 in
+        # 32 bits is 0.001 to 2^-24 / 0.001 of itself, under the root)
+        assert np.abs(tr.params() - (p - step)).max() <= 1e-2 * (16 * 2.0 ** -24 + 2.0 ** -24 / 0.001) * 1.01 + 2.0 ** -24 * np.abs(p).max()
+        p = tr.params().astype(np.float64)
+        assert tr.opt_state()[2] == t
+
+
+def test_teacher_and_student_together(B):
+    """A teacher acts on states drawn from its replay, its top actions train a student, which acts in turn: each loss is
+    the operator's on the student's Q-values of before, to the rounding of those."""
+    teacher = trainer(B, H=128, seed=1)
+    student = trainer(B, H=64, layered=True, seed=2)
+    for _ in range(10):
+        teacher.step()
+    u = torch.rand(64, device="cuda")
+    for step in range(5):
+        _, (s, *_) = teacher.replay.sample_gather(step, 64)
+        q, z = torch.empty((64, 30), device="cuda"), torch.empty((64, 30), device="cuda")
+        teacher.act(s, u, q=q)
+        value, index, lse = B.top_actions(q, 8, temperature=0.3)
+        before, _ = student.act(s, u, q=z)
+        want = B.distill_loss(z, value, index, teacher_lse=lse, teacher_temperature=0.3).mean().item()
+        student.distill_batch(s, value, index, teacher_lse=lse, teacher_temperature=0.3)
+        scale = 1 + z.abs().max().item()
+        assert abs(student.last()["loss"] - want) <= 16 * 2.0 ** -24 * (27 + 64 + 64) * scale
+        action, logp = student.act(s, u, temperature=0.3, top_k=8)
+        assert ((action >= 0) & (action < 30)).all() and (logp <= 0).all()
+
+
+def test_paths_refuse_what_they_cannot_do(B):
+    fast, slow = trainer(B), trainer(B, layered=True)
+    s = torch.randn((64, 27), device="cuda")
+    value, index, lse = B.top_actions(torch.randn((64, 30), device="cuda"), 5)
+    with pytest.raises(B.ReplayError, match="LAYERED"):
+        fast.distill_batch(s, value, index)
+    before = slow.params()
+    for bad in (dict(s=s[:63]), dict(s=s.double()), dict(index=index[:63]), dict(index=index.long()), dict(teacher=value.half()),
+                dict(weight=torch.ones(63, device="cuda")), dict(teacher_lse=lse.double())):
+        with pytest.raises(ValueError):
+            slow.distill_batch(**{"s": s, "teacher": value, "index": index, **bad})
+    for bad in (dict(student_temperature=0.0), dict(teacher_temperature=math.nan)):
+        with pytest.raises(B.ReplayError):
+            slow.distill_batch(s, value, index, **bad)
+    u = torch.rand(64, device="cuda")
+    for bad in (dict(s=s[:63]), dict(s=s.bfloat16()), dict(q=torch.empty((64, 29), device="cuda")),
+                dict(temperature=torch.ones(63, device="cuda"))):
+        with pytest.raises(ValueError):
+            slow.act(**{"s": s, "u": u, **bad})
+    with pytest.raises(B.ReplayError):
+        slow.act(s[:0], u[:0])
+    assert np.array_equal(slow.params(), before) and slow.opt_state()[2:] == (0, 0)

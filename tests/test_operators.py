@@ -135,3 +135,16 @@ def test_a_workspace_that_is_too_small_is_refused():
         assert need > 0
         assert call(None, 0) == B.RP_ENOMEM and call(0x1000, need - 1) == B.RP_ENOMEM and call(None, need) == B.RP_ENOMEM
         assert call(0x1010, need) == B.RP_ENOMEM and b"aligned" in lib.rp_last_error()
+
+
+def test_the_trainers_paths_check_their_arguments():
+    lib = B.lib()
+    cfg = B.TrainConfig(27, 256, 30, 128, B.RP_F32, 0, 1, 1, 1e-4, 0.99, 0.9, 0.999, 1e-8, 1)
+    size = lambda c, n: lib.train_act_workspace_bytes(C.byref(c), n)
+    assert size(cfg, 1) >= (256 + 256 + 30) * 4 and size(cfg, 1000) >= 1000 * (256 + 256 + 30) * 4
+    assert size(cfg, 0) == 0 and size(cfg, 2 ** 20 + 1) == 0
+    bad = B.TrainConfig(27, 100, 30, 128, B.RP_F32, 0, 1, 1, 1e-4, 0.99, 0.9, 0.999, 1e-8, 1)
+    assert size(bad, 4) == 0
+    how = B.Choice(1.0, 1.0, 0.0, 0, None, None, None, None)
+    assert lib.train_act(None, 4, P, C.byref(how), P, P, None, None, P, 1 << 20, None) == EINVAL
+    assert lib.train_distill_batch(None, P, C.byref(teacher()), None) == EINVAL

@@ -281,8 +281,10 @@ __device__ void sort_words(ChooseShared<W>& s, unsigned int count) {
 #pragma unroll
     for (int j = 0; j < kEach; ++j)
         if (j * 64 * W + tid < count) {
-            // (infinite ends share one bucket)
-            const unsigned int b = scale > 0.f ? min((unsigned int)((high - key_value(word_key(mine[j]))) * scale), kBuckets - 1u) : 0u;
+            // (equal logits go by their place in the row, infinite ends share one bucket)
+            const unsigned int b = scale > 0.f    ? min((unsigned int)((high - key_value(word_key(mine[j]))) * scale), kBuckets - 1u)
+                                   : range == 0.f ? word_index(mine[j]) / (kMaxActions / kBuckets)
+                                                  : 0u;
             at[j] = b << 16 | atomicAdd(&s.buckets[b], 1u);
         }
     __syncthreads();
@@ -317,7 +319,7 @@ __device__ void sort_words(ChooseShared<W>& s, unsigned int count) {
         if (j * 64 * W + tid < count) {
             const unsigned int from = s.buckets[at[j] >> 16], to = s.buckets[(at[j] >> 16) + 1u];
             unsigned int rank = from;
-#pragma unroll 1
+#pragma unroll 4
             for (unsigned int i = from; i < to; ++i) rank += w[i] > mine[j];
             at[j] = rank;
         }
@@ -331,7 +333,7 @@ __device__ void sort_words(ChooseShared<W>& s, unsigned int count) {
 // The elements that `in` takes, as words in LDS in any order; returns their number, which may pass kList (the
 // rest is not kept then).
 template <int W, typename Row, typename In>
-__device__ unsigned int gather_words(const Row& row, ChooseShared<W>& s, In in) {
+__device__ __forceinline__ unsigned int gather_words(const Row& row, ChooseShared<W>& s, In in) {
     if (threadIdx.x == 0) s.taken = 0;
     __syncthreads();
     row.each([&](float x, unsigned int i, int) {
@@ -573,7 +575,7 @@ __device__ __forceinline__ unsigned long long near_units(double z) {
 }
 
 template <int W, typename Row>
-__device__ void bin_weights(const Row& row, const Bins& bins, ChooseShared<W>& s) {
+__device__ __forceinline__ void bin_weights(const Row& row, const Bins& bins, ChooseShared<W>& s) {
     for (unsigned int i = threadIdx.x; i < kBins; i += 64 * W) s.hist[i] = 0;
     __syncthreads();
     const float least = bins.lo((double)(kBins - 1));
@@ -636,19 +638,11 @@ __device__ unsigned int find_bin(ChooseShared<W>& s, Reached reached) {
     return bin;
 }
 
-// The actions of bin b as words in LDS; false if they do not fit.
-template <int W, typename Row>
-__device__ bool list_bin(const Row& row, const Bins& bins, unsigned int b, ChooseShared<W>& s, unsigned int* count) {
-    const float lo = bins.lo((double)b), hi = bins.hi((double)b);
-    *count = gather_words<W>(row, s, [&](float x) { return x >= lo && x < hi; });
-    return *count <= kList;
-}
-
 // Of the `count` actions of bin b in LDS, the first in order with which the inclusive sum over the row reaches `target` (passes
 // it, if `past`), or the last of them if rounding has it otherwise: its word and that sum, in s.word and s.part[0].  A bin
 // holds some hundred actions of a long row, so a histogram of its parts comes before anything is sorted.
 template <int W>
-__device__ void locate(const Bins& bins, unsigned int b, unsigned int count, double target, bool past, float m, double inv_t,
+__device__ __forceinline__ void locate(const Bins& bins, unsigned int b, unsigned int count, double target, bool past, float m, double inv_t,
                        ChooseShared<W>& s) {
     const unsigned int tid = threadIdx.x;
     double before = b ? s.sums[b - 1u] : 0.0;
@@ -749,11 +743,10 @@ __device__ void locate(const Bins& bins, unsigned int b, unsigned int count, dou
 // From the inclusive sums over bins to the choice; false if a bin holds too many actions for LDS, or, by a rounding of the
 // sums, none.
 template <int W, typename Row>
-__device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned long long row, const RowChoice& c,
+__device__ __forceinline__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned long long row, const RowChoice& c,
                                  const Bins& bins, float m, ChooseShared<W>& s) {
     const unsigned int tid = threadIdx.x;
     double mass = s.sums[kBins - 1];
-    unsigned int count;
     // the sum over the actions that stay: each limit keeps the first so many, and the shorter one counts
     unsigned int bin_p = kBins, bin_m = kBins;
     // (the best action always stays, and the sum reaches its weight with it)
@@ -764,9 +757,18 @@ __device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned 
         bin_m = b < (double)kBins ? (unsigned int)fmax(b, 0.0) : kBins;
     }
     const unsigned int last = min(bin_p, bin_m);
-    if (last < kBins) {
-        if (!list_bin<W>(row_, bins, last, s, &count)) return false;
-        if (bin_m == last) {
+    const bool end = !(c.u < 1.f);
+    // first the bin where the actions that stay end, if there is a limit, then the one of the choice
+    auto round = [&](int pass) __attribute__((always_inline)) {
+        const double target = pass == 0 ? most : end ? mass : c.u > 0.f ? (double)c.u * mass : 0.0;
+        const bool past = pass == 1 && !end;
+        unsigned int bin = last;
+        if (pass) bin = find_bin<W>(s, [&](double v) { return past ? v > target : v >= target; });
+        const float lo = bins.lo((double)bin), hi = bins.hi((double)bin);
+        const unsigned int count = gather_words<W>(row_, s, [&](float x) { return x >= lo && x < hi; });
+        const bool find = pass == 1 || bin_p == last;
+        if (count > kList || (count == 0 && find)) return false;
+        if (pass == 0 && bin_m == last) {
             // (whole numbers: their sum does not depend on the order in which the list was filled)
             unsigned long long units = 0;
             for (unsigned int i = tid; i < count; i += 64 * W) {
@@ -777,19 +779,23 @@ __device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned 
             __syncthreads();
             mass = fmin(mass, fmax((last ? s.sums[last - 1u] : 0.0) + (double)units * (1.0 / kOne), 1.0));
         }
-        if (bin_p == last) {
-            if (count == 0) return false;
-            locate<W>(bins, last, count, most, false, m, c.inv_t, s);
-            mass = fmin(mass, s.part[0]);
+        if (find) {
+            locate<W>(bins, bin, count, target, past, m, c.inv_t, s);
+            if (pass == 0) mass = fmin(mass, s.part[0]);
             __syncthreads();
         }
+        return true;
+    };
+    if constexpr (W == 8) {
+        // (once in the code: twice, the compiler no longer keeps the eight loads of a thread in registers, 42 us instead of 30
+        // for 1000 x 32768; the others keep theirs and lose by the loop, 52 us instead of 45 for 4096 x 1000)
+#pragma unroll 1
+        for (int pass = last < kBins ? 0 : 1; pass < 2; ++pass)
+            if (!round(pass)) return false;
+    } else {
+        if (last < kBins && !round(0)) return false;
+        if (!round(1)) return false;
     }
-    // the choice
-    const bool end = !(c.u < 1.f);
-    const double drawn = end ? mass : c.u > 0.f ? (double)c.u * mass : 0.0;
-    const unsigned int bin = find_bin<W>(s, [&](double v) { return end ? v >= drawn : v > drawn; });
-    if (!list_bin<W>(row_, bins, bin, s, &count) || count == 0) return false;
-    locate<W>(bins, bin, count, drawn, !end, m, c.inv_t, s);
     if (tid == 0)
         put_choice(p, row, (int)word_index(s.word),
                    (float)(-logit_depth(m, key_value(word_key(s.word)), c.inv_t) - log(mass)));
@@ -798,7 +804,7 @@ __device__ bool choose_from_bins(const Row& row_, const ChooseArgs& p, unsigned 
 
 // One row, all of it at hand.
 template <int W, int SLOTS, typename T, typename Row>
-__device__ void choose_row(const Row& held, const ChooseArgs& p, unsigned long long row, ChooseShared<W>& s) {
+__device__ __forceinline__ void choose_row(const Row& held, const ChooseArgs& p, unsigned long long row, ChooseShared<W>& s) {
     const RowChoice c = row_choice(p, row);
     float slot[SLOTS];
     const float m = slot_max<W, SLOTS>(held, slot, s);
@@ -906,7 +912,7 @@ __device__ __forceinline__ void put_lse(const TopArgs& p, unsigned long long row
 }
 
 template <int W, int SLOTS, typename T, typename Row>
-__device__ void top_row(const Row& held, const TopArgs& p, unsigned long long row, const Global<T>* x, ChooseShared<W>& s) {
+__device__ __forceinline__ void top_row(const Row& held, const TopArgs& p, unsigned long long row, const Global<T>* x, ChooseShared<W>& s) {
     float slot[SLOTS];
     const float m = slot_max<W, SLOTS>(held, slot, s);
     unsigned int count = 0;

@@ -379,7 +379,7 @@ size_t rp_top_workspace_bytes(const rp_rows* logits, uint32_t k);
  * The k (1 .. min(n, 1024)) largest logits of every row, in the order of rp_choose_actions:
  * values[rows * k] in the logits' type and index[rows * k]; past the last allowed action -infinity and
  * -1.  lse[rows] (may be NULL): log sum_j exp(x_j / temperature) over the whole row, with
- * a finite temperature > 0 (-infinity for a row without an allowed action).  What a teacher
+ * a temperature of 1e-30 .. 1e30 (-infinity for a row without an allowed action).  What a teacher
  * writes down for rp_distill_loss.
  */
 rp_status rp_top_actions(const rp_rows* logits, uint32_t k, double temperature, void* values, int32_t* index,
@@ -394,8 +394,8 @@ typedef struct {
                                    A row of weight 0 is not read: loss 0, gradient 0                  */
     uint32_t k;
     uint32_t dtype;             /* of value: RP_F32 | RP_BF16                                         */
-    double temperature;         /* the teacher's, finite > 0                                          */
-    double student_temperature; /* finite > 0                                                         */
+    double temperature;         /* the teacher's, 1e-30 .. 1e30                                       */
+    double student_temperature; /* 1e-30 .. 1e30                                                      */
 } rp_teacher;
 
 /* Bytes of device workspace rp_distill_loss and rp_distill_grad need ((size_t)-1 if invalid). */

@@ -421,7 +421,7 @@ class Trainer:
         check_device_array(s, _TORCH_STATE[rc.state_dtype], rows * rc.state_dim, dev, "act: s")
         if q is not None:
             check_device_array(q, (torch.float32,), rows * self.cfg.num_actions, dev, "act: q")
-        with _On(s.device, stream):
+        with _on(s.device, stream):
             how, u, out = _choice("act", rows, s.device, u, temperature, top_k, top_p, min_p, out)
             nbytes = int(lib().train_act_workspace_bytes(C.byref(self.cfg), rows))
             ws = _alloc_bytes(nbytes, s.device)
@@ -571,16 +571,17 @@ def _logit_rows(t):
     return LogitRows(t.data_ptr(), t.shape[0], t.stride(0), t.shape[1], _LOGIT_DTYPE[t.dtype])
 
 
-class _On:
-    """The device of a call's tensors as the current one and, if a stream is given, that stream for what the
-    call allocates; nothing to do for most calls."""
+class _Nothing:
+    def __enter__(self):
+        pass
 
-    def __init__(self, device, stream):
-        self._hold = []
-        if device.index is not None and device.index != torch.cuda.current_device():
-            self._hold.append(torch.cuda.device(device))
-        if stream is not None:
-            self._hold.append(torch.cuda.stream(stream))
+    def __exit__(self, *error):
+        pass
+
+
+class _Where(_Nothing):
+    def __init__(self, *hold):
+        self._hold = hold
 
     def __enter__(self):
         for h in self._hold:
@@ -589,6 +590,18 @@ class _On:
     def __exit__(self, *error):
         for h in reversed(self._hold):
             h.__exit__(*error)
+
+
+_nothing = _Nothing()
+
+
+def _on(device, stream):
+    """The device of a call's tensors as the current one and, if a stream is given, that stream for what the
+    call allocates; nothing to do for most calls."""
+    here = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    if device.index is None or device.index == here:
+        return _nothing if stream is None else _Where(torch.cuda.stream(stream))
+    return _Where(torch.cuda.device(device)) if stream is None else _Where(torch.cuda.device(device), torch.cuda.stream(stream))
 
 
 def _workspace(nbytes, workspace, device, what):
@@ -616,7 +629,8 @@ def _choice(what, rows, dev, u, temperature, top_k, top_p, min_p, out):
         check_device_array(out[0], (torch.int32,), rows, dev, what + ": index")
         if out[1] is not None:
             check_device_array(out[1], (torch.float32,), rows, dev, what + ": logp")
-    return Choice(1.0 if t is None else t, 1.0 if p is None else p, 0.0 if m is None else m, 0 if k is None else k,
+    return Choice(1.0 if t is None else float(t), 1.0 if p is None else float(p), 0.0 if m is None else float(m),
+                  0 if k is None else int(k),
                   _dev(t_row), _dev(p_row), _dev(m_row), _dev(k_row)), u, out
 
 
@@ -626,7 +640,7 @@ def choose_actions(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ou
     Returns (index int32[rows], logp float32[rows]), in `out` if given."""
     check_rows(logits, "choose_actions: logits")
     rows, dev = logits.shape[0], logits.device
-    with _On(dev, stream):
+    with _on(dev, stream):
         how, u, out = _choice("choose_actions", rows, dev, u, temperature, top_k, top_p, min_p, out)
         x = _logit_rows(logits)
         hold, ws, nbytes = _workspace(lib().rp_choose_workspace_bytes(C.byref(x)), workspace, dev, "choose_actions")
@@ -640,7 +654,7 @@ def top_actions(logits, k, temperature=1.0, out=None, workspace=None, stream=Non
     rp_top_actions.  Returns (values [rows, k] in the logits' type, index int32[rows, k], lse float32[rows])."""
     check_rows(logits, "top_actions: logits")
     rows, dev = logits.shape[0], logits.device
-    with _On(dev, stream):
+    with _on(dev, stream):
         x = _logit_rows(logits)
         need = lib().rp_top_workspace_bytes(C.byref(x), k)
         hold, ws, nbytes = _workspace(need, workspace, dev, "top_actions")
@@ -680,7 +694,7 @@ def distill_loss(logits, teacher, index, weight=None, teacher_lse=None, student_
     rows, dev = logits.shape[0], logits.device
     x = _logit_rows(logits)
     t = _teacher(rows, dev, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_loss")
-    with _On(dev, stream):
+    with _on(dev, stream):
         hold, ws, nbytes = _workspace(lib().rp_distill_workspace_bytes(C.byref(x), t.k), workspace, dev, "distill_loss")
         out = torch.empty(rows, dtype=torch.float32, device=dev) if out is None else out
         check_device_array(out, (torch.float32,), rows, dev, "distill_loss: out")
@@ -697,7 +711,7 @@ def distill_grad(logits, teacher, index, weight=None, teacher_lse=None, student_
     rows, dev = logits.shape[0], logits.device
     x = _logit_rows(logits)
     t = _teacher(rows, dev, teacher, index, weight, teacher_lse, student_temperature, teacher_temperature, "distill_grad")
-    with _On(dev, stream):
+    with _on(dev, stream):
         hold, ws, nbytes = _workspace(lib().rp_distill_workspace_bytes(C.byref(x), t.k), workspace, dev, "distill_grad")
         if out is None:
             out = (torch.empty(rows, dtype=torch.float32, device=dev),

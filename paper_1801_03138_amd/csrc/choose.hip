@@ -1219,7 +1219,7 @@ __global__ __launch_bounds__(64 * W, 4) void choose_join_kernel(ChooseArgs p, Pi
             for (unsigned int j = 0; j < kBins / (64 * W); ++j) s.hist[j * 64 * W + tid] = sum[j];
             __syncthreads();
             sum_bins<W>(bins, m, s);
-            done = choose_from_bins<W>(BatchRow<W, 8, T>(global_in<T>(p.x.data) + row * p.x.stride, 0, p.x.n), p, row, choice, bins, m, s);
+            done = choose_from_bins<W>(ReadRow<W, 8, T>(global_in<T>(p.x.data) + row * p.x.stride, 0, p.x.n), p, row, choice, bins, m, s);
         }
     }
     if (!done) {
@@ -1398,7 +1398,7 @@ rp_status rp_top_actions(const rp_rows* logits, uint32_t k, double temperature, 
     const char* why = rp::logit_rows_fault(logits);
     RP_REQUIRE(!why, "rp_top_actions: %s", why);
     RP_REQUIRE(k >= 1 && k <= rp::kMaxTop && k <= logits->n, "rp_top_actions: k = %u, must be 1 .. min(n, 1024)", k);
-    RP_REQUIRE(temperature > 0.0 && std::isfinite(temperature), "rp_top_actions: the temperature must be finite and > 0");
+    RP_REQUIRE(rp::temperature_fits(temperature), "rp_top_actions: the temperature must be 1e-30 .. 1e30");
     if (logits->rows == 0) return RP_OK;
     why = rp::logit_data_fault(logits);
     RP_REQUIRE(!why, "rp_top_actions: %s", why);

@@ -42,7 +42,7 @@ struct MaxSum {
 
 // What a wavefront knows of the row's entries.
 struct EntryPart {
-    double tm, a, b, c;   // max of t / tt (REST: the teacher's log-sum-exp); sums of q' = exp(t / tt - tm), q' (t / tt - tm), q' z / ts
+    double tm, a, b, c;   // max of t (REST: unused); sums of q' = exp(d), q' d, q' (z - zm) / ts with d = log_weight(t)
     double z;             // sum of exp((z - zm) / ts), each action once
     float zm;
     unsigned int any;     // some entry is there with a logit above -infinity
@@ -90,6 +90,13 @@ __device__ __forceinline__ void load_entries(const DistillArgs& p, unsigned long
     }
 }
 
+// log of an entry's unnormalised weight: over `shift`, the largest of the teacher's logits, or (REST) its log-sum-exp.  The
+// difference comes before the division: a product less a product may be fused, and is then not zero for the largest.
+template <bool REST>
+__device__ __forceinline__ double log_weight(const DistillArgs& p, float t, double shift) {
+    return REST ? (double)t * p.inv_tt - shift : ((double)t - shift) * p.inv_tt;
+}
+
 // Sums over the wavefront's share of the entries.
 template <int W, bool REST>
 __device__ __forceinline__ void sum_entries(const DistillArgs& p, unsigned long long row, Entries en, DistillShared<W>& s) {
@@ -107,13 +114,13 @@ __device__ __forceinline__ void sum_entries(const DistillArgs& p, unsigned long 
         tm = wave_reduce(tm, MaxOp{});
         r.zm = wave_reduce(r.zm, MaxOp{});
         r.any = tm > -INFINITY;
-        r.tm = REST ? (double)global_in<float>(p.teacher_lse)[row] : (double)tm * p.inv_tt;
-        const double tm0 = REST || r.any ? r.tm : 0.0, zm0 = r.zm > -INFINITY ? (double)r.zm : 0.0;
+        r.tm = (double)tm;
+        const double tm0 = REST ? (double)global_in<float>(p.teacher_lse)[row] : r.any ? r.tm : 0.0, zm0 = r.zm > -INFINITY ? (double)r.zm : 0.0;
         const bool twice = s.twice;
 #pragma unroll 1
         for (unsigned int e = tid; e < k; e += 64 * W) {
             if (en.act[e] < 0) continue;
-            const double d = (double)en.t[e] * p.inv_tt - tm0, z = (double)en.z[e];
+            const double d = log_weight<REST>(p, en.t[e], tm0), z = (double)en.z[e];
             bool first = true;
             if (twice)
 #pragma unroll 1
@@ -128,7 +135,7 @@ __device__ __forceinline__ void sum_entries(const DistillArgs& p, unsigned long 
                     r.a += v;
                     if (!(v == 0.0)) {
                         r.b += v * d;
-                        r.c += v * z * p.inv_ts;
+                        r.c += v * ((z - zm0) * p.inv_ts);
                     }
                 }
             }
@@ -259,12 +266,14 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     const double shift = REST ? (double)global_in<float>(p.teacher_lse)[row] : any ? tm : 0.0;
     double from = quarter == 0 ? (own_x > -INFINITY ? ((double)own_x - m0) * p.inv_ts : 0.0)
                   : quarter == 1 ? (own_z > -INFINITY ? ((double)own_z - m0) * p.inv_ts : 0.0)
-                                 : (!REST && own_any ? own_t - shift : 0.0);
+                                 : (!REST && own_any ? (own_t - shift) * p.inv_tt : 0.0);
     const double factor = exp(from);
     double first = quarter == 0 ? (row_here ? x.s : 0.0) : quarter == 1 ? (part_here ? r.z : 0.0) : (part_here ? r.a : 0.0);
     double b = part_here ? r.b : 0.0, c = part_here ? r.c : 0.0;
     // (q' (t - tm) from a wavefront's own maximum to the row's)
     if (!REST && quarter >= 2u) b = first == 0.0 ? 0.0 : (b + first * from) * factor;
+    // (and q' (z - zm) from its own student's maximum to the row's)
+    c = first == 0.0 ? 0.0 : c + first * (own_z > -INFINITY ? ((double)own_z - m0) * p.inv_ts : 0.0);
     if (!REST) c = factor == 0.0 ? 0.0 : c * factor;
     first = quarter_sum(first == 0.0 ? 0.0 : first * factor);
     b = __shfl(quarter_sum(b), 32, 64);
@@ -275,7 +284,7 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     const double logs = log(lane == 0   ? total
                             : lane == 1 ? (REST ? 1.0 - a : a)
                                         : (p_in < 0.5 ? 1.0 - p_in : p_rest));
-    const double log_total = __shfl(logs, 0, 64) + m0 * p.inv_ts, log_a = __shfl(logs, 1, 64), log_rest = __shfl(logs, 2, 64);
+    const double log_total = __shfl(logs, 0, 64), log_a = __shfl(logs, 1, 64), log_rest = __shfl(logs, 2, 64);
     double loss, q_scale = 1.0, inside = 1.0, outside = 1.0;
     if (!REST) {
         q_scale = 1.0 / a;
@@ -333,7 +342,7 @@ __device__ __forceinline__ void put_gradient(const Row& row, Global<T>* g, const
 }
 
 // The gradient of the actions among begin .. end that have an entry.
-template <int W, typename T>
+template <int W, typename T, bool REST>
 __device__ __forceinline__ void put_entries(const DistillArgs& p, Global<T>* g, Entries en, unsigned int begin, unsigned int end,
                                             const RowScalars& o, bool twice) {
     const unsigned int k = p.k;
@@ -341,7 +350,7 @@ __device__ __forceinline__ void put_entries(const DistillArgs& p, Global<T>* g, 
     for (unsigned int e = threadIdx.x; e < k; e += 64 * W) {
         const unsigned int a = (unsigned int)en.act[e];
         if (a < begin || a >= end) continue;   // (-1 is beyond any end)
-        double q = wide_exp((double)en.t[e] * p.inv_tt - o.shift) * o.q_scale;
+        double q = wide_exp(log_weight<REST>(p, en.t[e], o.shift)) * o.q_scale;
         if (twice) {   // the first of an action's entries writes, with the sum of all
             bool first = true;
             q = 0.0;
@@ -349,7 +358,7 @@ __device__ __forceinline__ void put_entries(const DistillArgs& p, Global<T>* g, 
             for (unsigned int f = 0; f < k; ++f)
                 if (en.act[f] == (int)a) {
                     first &= f >= e;
-                    q += wide_exp((double)en.t[f] * p.inv_tt - o.shift) * o.q_scale;
+                    q += wide_exp(log_weight<REST>(p, en.t[f], o.shift)) * o.q_scale;
                 }
             if (!first) continue;
         }
@@ -431,7 +440,7 @@ __global__ __launch_bounds__(64) void distill_wave_kernel(DistillArgs p) {
             if (i < n) store_gradient(g + i, factor * weight_of(held.v[j], o.m, p.c2));
         }
         __syncthreads();   // (an action with an entry is written again)
-        if (o.state == 0) put_entries<1, T>(p, g, en, 0, n, o, s.twice != 0);
+        if (o.state == 0) put_entries<1, T, REST>(p, g, en, 0, n, o, s.twice != 0);
     }
 }
 
@@ -446,7 +455,7 @@ __device__ __forceinline__ void distill_row(const DistillArgs& p, unsigned long 
     load_entries<W, T, TT, REST || GRAD>(p, row, x, nullptr, 0, n, en, named, s);
     __syncthreads();
     sum_entries<W, REST>(p, row, en, s);
-    const MaxSum mine = sum_row<REST, T>(held, ReadRow<W, T, 1>(x, 0, n), 0, named, p.c2);
+    const MaxSum mine = sum_row<REST, T>(held, ReadRow<W, 1, T, false>(x, 0, n), 0, named, p.c2);
     if ((tid & 63u) == 0) s.row[tid >> 6] = mine;
     __syncthreads();
     if (tid < 64) finish_row<REST>(p, row, weight, s.part, W, s.row, W, &s.out);
@@ -454,7 +463,7 @@ __device__ __forceinline__ void distill_row(const DistillArgs& p, unsigned long 
     __syncthreads();
     put_gradient<T>(held, g, s.out, p.c2);
     __syncthreads();   // (an action with an entry is written again)
-    if (s.out.state == 0) put_entries<W, T>(p, g, en, 0, n, s.out, s.twice != 0);
+    if (s.out.state == 0) put_entries<W, T, REST>(p, g, en, 0, n, s.out, s.twice != 0);
 }
 
 // One workgroup of W wavefronts per row, held in registers (NV > 0) or read again for each of three passes.  LDS
@@ -479,7 +488,7 @@ __global__ __launch_bounds__(64 * W, EU) void distill_kernel(DistillArgs p) {
         } else if constexpr (NV > 0) {
             distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, HeldRow<W, NV, T, false>(x, 0, n), lds, words, en, s);
         } else {
-            distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, ReadRow<W, T>(x, 0, n), lds, words, en, s);
+            distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, ReadRow<W, W == 8 ? 8 : 4, T, false>(x, 0, n), lds, words, en, s);
         }
     }
 }
@@ -537,7 +546,7 @@ __global__ __launch_bounds__(64 * W, 4) void distill_piece_kernel(DistillArgs p,
         }
     }
     __syncthreads();
-    const ReadRow<W, T> read(x, begin, end);
+    const ReadRow<W, 4, T, false> read(x, begin, end);
     const MaxSum mine = sum_row<REST, T>(read, read, begin, named, p.c2);
     if ((tid & 63u) == 0) part[tid >> 6] = mine;
     __syncthreads();
@@ -594,9 +603,9 @@ __global__ __launch_bounds__(64 * W, 4) void distill_join_kernel(DistillArgs p, 
     if (tid < 64) finish_row<REST>(p, row, weight, s.part, W, s.row, 1, &s.out, piece == 0);
     if (!GRAD) return;
     __syncthreads();
-    put_gradient<T>(ReadRow<W, T>(x, begin, end), g, s.out, p.c2);
+    put_gradient<T>(ReadRow<W, 4, T, false>(x, begin, end), g, s.out, p.c2);
     __syncthreads();   // (an action with an entry is written again)
-    if (s.out.state == 0) put_entries<W, T>(p, g, en, begin, end, s.out, s.twice != 0);
+    if (s.out.state == 0) put_entries<W, T, REST>(p, g, en, begin, end, s.out, s.twice != 0);
 }
 
 template <typename T, typename TT, bool REST, bool GRAD>
@@ -623,7 +632,8 @@ hipError_t launch_rows(const DistillArgs& a, void* workspace, hipStream_t st) {
         if (n <= HeldRow<1, 4, T>::kMost) distill_kernel<1, 4, 4, T, TT, REST, GRAD><<<blocks, 64, lds, st>>>(a);
         else if (n <= HeldRow<2, 8, T>::kMost) distill_kernel<2, 8, 3, T, TT, REST, GRAD><<<blocks, 128, lds, st>>>(a);
         else if (n <= HeldRow<4, 8, T>::kMost) distill_kernel<4, 8, 4, T, TT, REST, GRAD><<<blocks, 256, lds, st>>>(a);
-        else if (n <= HeldRow<4, 16, T>::kMost) distill_kernel<4, 16, 3, T, TT, REST, GRAD><<<blocks, 256, lds, st>>>(a);
+        else if (n <= HeldRow<4, 16, T>::kMost) distill_kernel<4, 16, 4, T, TT, REST, GRAD><<<blocks, 256, lds, st>>>(a);
+        else if (n <= HeldRow<8, 16, T>::kMost) distill_kernel<8, 16, 4, T, TT, REST, GRAD><<<blocks, 512, lds, st>>>(a);
         else distill_kernel<8, 0, 4, T, TT, REST, GRAD><<<blocks, 512, lds, st>>>(a);
     }
     return hipGetLastError();
@@ -643,9 +653,8 @@ rp_status distill_rows(const char* what, const rp_rows* logits, const rp_teacher
     RP_REQUIRE(teacher, "%s: null teacher", what);
     RP_REQUIRE(teacher->k >= 1 && teacher->k <= kMaxTop, "%s: k = %u, must be 1 .. 1024", what, teacher->k);
     RP_REQUIRE(teacher->dtype == RP_F32 || teacher->dtype == RP_BF16, "%s: the teacher's logits must be RP_F32 or RP_BF16", what);
-    RP_REQUIRE(teacher->temperature > 0.0 && std::isfinite(teacher->temperature) && teacher->student_temperature > 0.0 &&
-                   std::isfinite(teacher->student_temperature),
-               "%s: temperatures must be finite and > 0", what);
+    RP_REQUIRE(temperature_fits(teacher->temperature) && temperature_fits(teacher->student_temperature),
+               "%s: temperatures must be 1e-30 .. 1e30", what);
     if (logits->rows == 0) return RP_OK;
     why = logit_data_fault(logits);
     RP_REQUIRE(!why, "%s: %s", what, why);

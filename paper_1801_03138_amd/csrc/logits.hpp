@@ -115,9 +115,9 @@ struct HeldRow {
     }
 };
 
-// The same interface over memory, for rows that registers do not hold: every pass reads the row again (and `each_load`
-// does not mask).
-template <int W, typename T, int UNROLL = 4>
+// The same interface over memory, for rows that registers do not hold: every pass reads the row again, NV loads a thread at a
+// time, all under way before the first is used.
+template <int W, int NV, typename T, bool MASK = true>
 struct ReadRow {
     static constexpr bool kHeld = false;
     const Global<T>* x;
@@ -125,39 +125,13 @@ struct ReadRow {
     __device__ __forceinline__ ReadRow(const Global<T>* x_, unsigned int begin_, unsigned int end_) : x(x_), begin(begin_), end(end_) {}
     template <typename F>
     __device__ __forceinline__ void each_load(F f) const {
-        constexpr unsigned int kStep = 64u * W * kPerLoad<T>;
-#pragma unroll UNROLL
-        for (unsigned int i = begin + threadIdx.x * kPerLoad<T>; i < end; i += kStep) {
-            const unsigned int at = load_place<T>(i, end);
-            f(*(const Global<u32x4_any>*)(x + at), at, i - at);
-        }
-    }
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {
-        constexpr unsigned int kStep = 64u * W * kPerLoad<T>;
-#pragma unroll UNROLL
-        for (unsigned int i = begin + threadIdx.x * kPerLoad<T>; i < end; i += kStep) {
-            const unsigned int at = load_place<T>(i, end);
-            u32x4 raw = *(const Global<u32x4_any>*)(x + at);
-            mask_moved<T>(raw, i, at);
-#pragma unroll
-            for (int e = 0; e < (int)kPerLoad<T>; ++e) f(element<T>(raw, e), at + e, e);
-        }
-    }
-};
-
-// The same, NV loads a thread at a time, all under way before the first is used: for passes whose loop the compiler does not
-// unroll.
-template <int W, int NV, typename T>
-struct BatchRow {
-    const Global<T>* x;
-    unsigned int begin, end;
-    __device__ __forceinline__ BatchRow(const Global<T>* x_, unsigned int begin_, unsigned int end_) : x(x_), begin(begin_), end(end_) {}
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {
-        constexpr unsigned int kMost = HeldRow<W, NV, T>::kMost;
 #pragma unroll 1
-        for (unsigned int at = begin; at < end; at += kMost) HeldRow<W, NV, T>(x, at, min(at + kMost, end)).each(f);
+        for (unsigned int at = begin; at < end; at += HeldRow<W, NV, T, MASK>::kMost) HeldRow<W, NV, T, MASK>(x, at, end).each_load(f);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll 1
+        for (unsigned int at = begin; at < end; at += HeldRow<W, NV, T, MASK>::kMost) HeldRow<W, NV, T, MASK>(x, at, end).each(f);
     }
 };
 
@@ -241,6 +215,8 @@ inline const char* logit_data_fault(const rp_rows* r) {
     if (reinterpret_cast<uintptr_t>(r->data) & (r->dtype == RP_BF16 ? 1u : 3u)) return "logits not aligned to their type";
     return nullptr;
 }
+// Temperatures of losses and log-sum-exps: within these ends 1 / t and log2(e) / t are numbers in 32 bits.
+inline bool temperature_fits(double t) { return t >= 1e-30 && t <= 1e30; }
 inline const char* workspace_fault(const void* workspace, size_t bytes, size_t need) {
     if (need == 0) return nullptr;
     if (!workspace || bytes < need) return "the workspace is too small";

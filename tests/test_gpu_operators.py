@@ -425,6 +425,46 @@ def test_the_same_call_gives_the_same_bits(B):
             assert all(torch.equal(a, b) for a, b in zip(calls(), want))
 
 
+def test_extreme_temperatures(B):
+    """At the ends of the allowed range: the teacher's and the student's best actions alone, or all alike."""
+    rng = np.random.default_rng(4)
+    for n in (30, 3000, 50_000):
+        g, x = table(rng, 3, n, "f32")
+        value, index, _ = entries(rng, x, 4, "f32", short=0.0)
+        tv, idx = torch.from_numpy(value.astype(np.float32)).cuda(), torch.from_numpy(index).cuda()
+        loss, grad = B.distill_grad(g, tv, idx, student_temperature=1e30, teacher_temperature=1e30)
+        # (uniform over the entries against uniform over n; the gradient, of size 1e-30, is a number)
+        assert np.abs(loss.cpu().numpy() - math.log(n / 4)).max() <= 2.0 ** -22 * (math.log(n) + 4) and torch.isfinite(grad).all()
+        loss, grad = B.distill_grad(g, tv, idx, student_temperature=1.0, teacher_temperature=1e-30)
+        first = np.array([ref.log_sum_exp(r) - r[i] for r, i in zip(x, index[:, 0])])
+        assert np.abs(loss.cpu().numpy() - first).max() <= 2.0 ** -22 * (math.log(n) + 4 + np.abs(first).max())
+        # the student at its coldest: no loss where it agrees with a single entry, else the difference / 1e-30
+        for at in (x.argmax(1), x.argmin(1)):
+            loss, grad = B.distill_grad(g, tv[:, :1].contiguous(), torch.from_numpy(at.astype(np.int32))[:, None].cuda(),
+                                        student_temperature=1e-30)
+            far = (x.max(1) - x[np.arange(3), at]) / 1e-30
+            assert np.abs(loss.double().cpu().numpy() - far).max() <= 2.0 ** -23 * far.max()
+        for t in (1e-30, 1e30):
+            _, top, lse = B.top_actions(g, 3, temperature=t)
+            best = x.max(1)
+            if t == 1e30:
+                assert np.abs(lse.cpu().numpy() - math.log(n)).max() <= 2.0 ** -22 * (math.log(n) + 4)
+            else:
+                assert np.abs(lse.double().cpu().numpy() / (best / t) - 1).max() <= 2.0 ** -23
+        for t in (1e-300, 1e-40, 1e40, 1e300):
+            u = draw_u(rng, 3)
+            index2, logp = B.choose_actions(g, torch.from_numpy(u).cuda(), temperature=t)
+            check_choice(x, u, {"temperature": t}, index2, logp)
+
+
+def test_settings_may_be_numbers_of_other_kinds(B):
+    g, x = table(np.random.default_rng(3), 2, 40, "f32")
+    u = torch.rand(2, device="cuda")
+    a = B.choose_actions(g, u, temperature=1, top_k=np.int32(5), top_p=np.float32(0.5), min_p=0)
+    b = B.choose_actions(g, u, temperature=1.0, top_k=5, top_p=0.5)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 def test_a_table_beyond_4_gib(B):
     """Offsets of the last rows pass 32 bits, in elements and in bytes."""
     n = 262_144

@@ -79,7 +79,7 @@ def test_settings_out_of_range_are_refused():
     for k in (0, 31, 1025):
         assert top(rows(), k=k) == EINVAL
     assert top(rows(n=4000, stride=4000), k=1025) == EINVAL
-    for t in (0.0, -1.0, math.inf, math.nan):
+    for t in (0.0, -1.0, math.inf, math.nan, 1e-31, 1e31):
         assert top(rows(), temperature=t) == EINVAL
         assert loss(rows(), teacher(temperature=t)) == EINVAL
         assert grad(rows(), teacher(student_temperature=t)) == EINVAL
@@ -128,7 +128,12 @@ def test_the_binding_checks_tensors():
 def test_a_workspace_that_is_too_small_is_refused():
     lib = B.lib()
     x = rows(rows=2, n=200_000, stride=200_000)
-    for need, call in ((lib.rp_distill_workspace_bytes(C.byref(x), 8),
+    how = B.Choice(1.0, 1.0, 0.0, 0, None, None, None, None)
+    for need, call in ((lib.rp_choose_workspace_bytes(C.byref(x)),
+                        lambda ws, b: lib.rp_choose_actions(C.byref(x), C.byref(how), P, P, None, ws, b, None)),
+                       (lib.rp_top_workspace_bytes(C.byref(x), 8),
+                        lambda ws, b: lib.rp_top_actions(C.byref(x), 8, 1.0, P, P, None, ws, b, None)),
+                       (lib.rp_distill_workspace_bytes(C.byref(x), 8),
                         lambda ws, b: lib.rp_distill_loss(C.byref(x), C.byref(teacher()), P, ws, b, None)),
                        (lib.rp_distill_workspace_bytes(C.byref(x), 8),
                         lambda ws, b: lib.rp_distill_grad(C.byref(x), C.byref(teacher()), P, 0x10000000, 200_000, ws, b, None))):

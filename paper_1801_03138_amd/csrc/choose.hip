@@ -1,5 +1,18 @@
 // Choosing actions from rows of logits (temperature, top-k, top-p, min-p, given random numbers) and a
 // row's top actions with its log-sum-exp.
+//
+// Both are about the order of a row by falling logit, of which only the front matters: nothing is sorted but the few
+// actions around the places in question.  The least work is one reading of the row (HBM at 5.1 TB/s).  By length and number of
+// rows:
+//  - up to 64 actions: one wavefront, an action a lane; a lane finds its place by comparing with all (choose_wave_kernel).
+//  - up to 16,384 / 32,768 actions in 32 / 16 bits: one workgroup that holds the row in registers, so that it is read once
+//    (choose_kernel, top_kernel).
+//  - longer rows, and few rows of more than 8192: a launch for pieces of the row, one that joins them.
+// Top-k (up to 1024) and the best action: the k-th largest of the maxima of 1024 to 4096 slices of the row is a lower bound of
+// the k-th largest logit and close to it; what is not below it is sorted in LDS.  All actions: a histogram of the
+// weights, 2048 bins to 40 temperatures below the maximum; only bins where a sum ends are listed.  What these cannot take (more than
+// 1024 kept by top-k, more than 2048 actions in a bin or above the bound, +infinity) is found by binary search over the
+// values, a pass over the row for each step.
 #include "logits.hpp"
 
 namespace rp {
@@ -835,6 +848,9 @@ __device__ __forceinline__ void choose_row(const Row& held, const ChooseArgs& p,
     }
 }
 
+// Eight wavefronts with eight loads each for long rows: 16 wavefronts of four and 4 of sixteen take 78 and 74 us for 66 at
+// 1000 x 32768 bf16 top-p, 38 and 34 for 30 at top-k.  What bounds it is not HBM (2.2 TB/s at top-k) but the instructions per
+// element: decoding, comparing, and without top-k some twenty in 64 bits and an LDS atomic for the weight.
 template <int W, int NV, int EU, typename T>
 __global__ __launch_bounds__(64 * W, EU) void choose_kernel(ChooseArgs p) {
     __shared__ ChooseShared<W> s;
@@ -931,6 +947,8 @@ __device__ __forceinline__ void top_row(const Row& held, const TopArgs& p, unsig
     put_top<W, T>(p, row, s.words, min(count, p.k));
 }
 
+// 2048 x 32768 bf16, k = 64: 47 us, 2.9 TB/s; four workgroups a compute unit, of which each takes in turn its loads and three passes
+// over registers (maxima, candidates, exponentials: about twelve instructions and an exp per element).
 template <int W, int NV, int EU, typename T>
 __global__ __launch_bounds__(64 * W, EU) void top_kernel(TopArgs p) {
     __shared__ ChooseShared<W> s;
@@ -959,49 +977,48 @@ __device__ __forceinline__ unsigned long long lanes_before(unsigned int key, uns
     return before;
 }
 
+// (5.9 us for one row of 30, 6.9 for 128 with settings of their own: two trips to memory, and the chains of 30 sums, exp and log)
 template <typename T>
 __global__ __launch_bounds__(256) void choose_wave_kernel(ChooseArgs p) {
     const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
     const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned long long row = workgroup_row() * 4u + wave;
     if (row >= p.x.rows) return;
-    {
-        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
-        const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
-        const RowChoice c = row_choice(p, row);
-        const long long k = p.row_top_k ? (long long)p.row_top_k[row] : p.top_k;
-        const unsigned long long before_me = lanes_before(order_key(v), n);
-        const unsigned int rank = __popcll(before_me);
-        const bool allowed = v > -INFINITY;
-        const float m = wave_reduce(v, MaxOp{});
-        if (m == -INFINITY) {
-            if (lane == 0) put_choice(p, row, -1, 0.f);
-            return;
-        }
-        if (c.greedy) {
-            if (rank == 0) put_choice(p, row, (int)lane, 0.f);
-            return;
-        }
-        const double w = allowed && (k <= 0 || (long long)rank < k) ? exp(-logit_depth(m, v, c.inv_t)) : 0.0;
-        double before = 0.0, total = 0.0;
-        for (unsigned int j = 0; j < n; ++j) {
-            const double other = lane_value(w, (int)j);
-            total += other;
-            before += before_me >> j & 1ull ? other : 0.0;
-        }
-        bool stays = w > 0.0;
-        if (c.top_p < 1.0) stays &= before < c.top_p * total;
-        if (c.min_p > 0.0) stays &= w >= c.min_p;
-        stays |= rank == 0;
-        const double upto = before + w;
-        const double mass = wave_reduce(stays ? upto : 0.0, MaxOp{});
-        const double drawn = c.u > 0.f ? (double)c.u * mass : 0.0;
-        // the first in order whose sum passes the drawn one, else the last that stays
-        const bool hit = stays && upto > drawn;
-        const unsigned int first = wave_reduce(hit ? rank : 64u, MinOp{});
-        const unsigned int at = first < 64u ? first : wave_reduce(stays ? rank : 0u, MaxOp{});
-        if (rank == at) put_choice(p, row, (int)lane, (float)(-logit_depth(m, v, c.inv_t) - log(mass)));
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
+    const RowChoice c = row_choice(p, row);
+    const long long k = p.row_top_k ? (long long)p.row_top_k[row] : p.top_k;
+    const unsigned long long before_me = lanes_before(order_key(v), n);
+    const unsigned int rank = __popcll(before_me);
+    const bool allowed = v > -INFINITY;
+    const float m = wave_reduce(v, MaxOp{});
+    if (m == -INFINITY) {
+        if (lane == 0) put_choice(p, row, -1, 0.f);
+        return;
     }
+    if (c.greedy) {
+        if (rank == 0) put_choice(p, row, (int)lane, 0.f);
+        return;
+    }
+    const double w = allowed && (k <= 0 || (long long)rank < k) ? exp(-logit_depth(m, v, c.inv_t)) : 0.0;
+    double before = 0.0, total = 0.0;
+    for (unsigned int j = 0; j < n; ++j) {
+        const double other = lane_value(w, (int)j);
+        total += other;
+        before += before_me >> j & 1ull ? other : 0.0;
+    }
+    bool stays = w > 0.0;
+    if (c.top_p < 1.0) stays &= before < c.top_p * total;
+    if (c.min_p > 0.0) stays &= w >= c.min_p;
+    stays |= rank == 0;
+    const double upto = before + w;
+    const double mass = wave_reduce(stays ? upto : 0.0, MaxOp{});
+    const double drawn = c.u > 0.f ? (double)c.u * mass : 0.0;
+    // the first in order whose sum passes the drawn one, else the last that stays
+    const bool hit = stays && upto > drawn;
+    const unsigned int first = wave_reduce(hit ? rank : 64u, MinOp{});
+    const unsigned int at = first < 64u ? first : wave_reduce(stays ? rank : 0u, MaxOp{});
+    if (rank == at) put_choice(p, row, (int)lane, (float)(-logit_depth(m, v, c.inv_t) - log(mass)));
 }
 
 template <typename T>
@@ -1010,28 +1027,29 @@ __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs p) {
     const unsigned int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned long long row = workgroup_row() * 4u + wave;
     if (row >= p.x.rows) return;
-    {
-        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
-        const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
-        const unsigned int rank = __popcll(lanes_before(order_key(v), n));
-        const unsigned int allowed = __popcll(__ballot(v > -INFINITY));
-        if (rank < p.k && lane < n) {
-            const unsigned long long at = row * p.k + rank;
-            store_value(global_out<T>(p.values) + at, v);
-            p.index[at] = rank < allowed ? (int)lane : -1;
-        }
-        if (p.lse) {
-            const float m = wave_reduce(v, MaxOp{});
-            const double w = m > -INFINITY && m < INFINITY ? (double)__builtin_amdgcn_exp2f((v - m) * p.c2) : 0.0;
-            const double total = wave_reduce(w, SumOp{});
-            if (lane == 0) p.lse[row] = m == INFINITY || m == -INFINITY ? m : (float)((double)m * p.inv_t + log(total));
-        }
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    const float v = lane < n ? clean_logit(logit_value(x + lane)) : -INFINITY;
+    const unsigned int rank = __popcll(lanes_before(order_key(v), n));
+    const unsigned int allowed = __popcll(__ballot(v > -INFINITY));
+    if (rank < p.k && lane < n) {
+        const unsigned long long at = row * p.k + rank;
+        store_value(global_out<T>(p.values) + at, v);
+        p.index[at] = rank < allowed ? (int)lane : -1;
+    }
+    if (p.lse) {
+        const float m = wave_reduce(v, MaxOp{});
+        const double w = m > -INFINITY && m < INFINITY ? (double)__builtin_amdgcn_exp2f((v - m) * p.c2) : 0.0;
+        const double total = wave_reduce(w, SumOp{});
+        if (lane == 0) p.lse[row] = m == INFINITY || m == -INFINITY ? m : (float)((double)m * p.inv_t + log(total));
     }
 }
 
 // ------------------------------------------------------------------------------ rows in pieces of a workgroup each
 // Long rows, and few ones: a launch brings each piece of a row to its candidates or to its histogram of weights, in the
-// workspace; a second one, a workgroup a row, joins them.
+// workspace; a second one, a workgroup a row, joins them.  The histograms' bins lie on multiples of one width, so a piece needs
+// no other's maximum.  us of the two launches: 1 x 131072 bf16 top-k 9 + 8; 37 x 50021 fp32 top-p 8 + 25, 256 x 131072 bf16 with
+// settings of their own 30 + 36: where there is no top-k, the join reads its row again for each of the one or two bins it lists,
+// on one compute unit.
 struct Pieces {
     unsigned int count, length;   // of a row; the last piece takes what is left
 };
@@ -1252,7 +1270,9 @@ __global__ __launch_bounds__(64 * W, 4) void top_join_kernel(TopArgs p, Pieces c
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-// How a row is cut: not at all where a workgroup's registers hold it and there are enough rows to fill the compute units.
+// How a row is cut: not at all where a workgroup's registers hold it and there are enough rows to fill the compute units, or the
+// row is too short for a second launch to pay.  (Pieces of 4096 instead of 8192 at least: 9 x 100003 top 500 47 us for the join
+// alone, which has to take in twice the candidates.)
 template <typename T>
 Pieces pieces_of(unsigned long long rows, unsigned int n) {
     const unsigned int held = HeldRow<8, 8, T>::kMost;

@@ -1,4 +1,15 @@
 // Distillation from a teacher's top logits: the loss of every row and the gradient of the student's logits.
+//
+// With m the row's maximum, w_i = exp((x_i - m) / ts) and their sum S the gradient is w_i times one number per row, but for the
+// at most 1024 actions with an entry, which are written again.  So a row needs a maximum, a sum, and for the gradient a second
+// exponential per element: HBM bounds it as long as the row is read once and written once, from registers.  Sums over a row
+// are held in 64 bits from one load to the next, exponentials in 32; entries and row scalars are in 64, since the loss is a
+// small difference of large logarithms.  The teacher's mass outside its entries is set against the sum over the other
+// actions, which is made directly (a bit per action in LDS tells which they are), not as a difference.
+//
+// 4096 x 32768 bf16, k = 64, a tenth of the rows of weight 0: 116 to 121 us, 4.2 to 4.4 TB/s of the 5.1 of a copy (the first kernel,
+// three passes over memory: 504).  Variants by wavefronts a row: the fewest that hold it, as rows that wait for memory
+// or for their chain of scalars are covered by others: 4096 x 1000 fp32 30 us with four wavefronts, 17 with one.
 #include "logits.hpp"
 
 namespace rp {
@@ -397,51 +408,49 @@ __global__ __launch_bounds__(64) void distill_wave_kernel(DistillArgs p) {
                      reinterpret_cast<float*>(lds + kWords + 2u * k)};
     const unsigned long long row = workgroup_row();
     if (row >= p.x.rows) return;
-    {
-        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
-        Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
-        const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
-        if (weight == 0.f) {
-            if (lane == 0) p.loss[row] = 0.f;
-            if (GRAD) put_zeros<1, T>(g, n);
-            return;
-        }
-        const ShortRow<NV, T> held(x, n);
-        if (lane < kWords) named[lane] = 0;
-        if (lane == 0) s.twice = 0;
-        __syncthreads();
-        load_entries<1, T, TT, true>(p, row, x, nullptr, 0, n, en, named, s);
-        __syncthreads();
-        sum_entries<1, REST>(p, row, en, s);
-        float m = -INFINITY;
-        bool out[NV];
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const unsigned int i = lane + 64u * j;
-            out[j] = REST && (named[i >> 5] >> (i & 31u) & 1u);
-            m = fmaxf(m, out[j] ? -INFINITY : held.v[j]);
-        }
-        m = wave_reduce(m, MaxOp{});
-        const float m0 = m > -INFINITY ? m : 0.f;
-        double sum = 0.0;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) sum += out[j] ? 0.0 : (double)weight_of(held.v[j], m0, p.c2);
-        sum = wave_reduce(sum, SumOp{});
-        if (lane == 0) s.row[0] = MaxSum{m, sum};
-        __syncthreads();
-        finish_row<REST>(p, row, weight, s.part, 1, s.row, 1, &s.out);
-        if (!GRAD) return;
-        __syncthreads();
-        const RowScalars o = s.out;
-        const float factor = o.state == 1u ? 0.f : o.factor;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const unsigned int i = lane + 64u * j;
-            if (i < n) store_gradient(g + i, factor * weight_of(held.v[j], o.m, p.c2));
-        }
-        __syncthreads();   // (an action with an entry is written again)
-        if (o.state == 0) put_entries<1, T, REST>(p, g, en, 0, n, o, s.twice != 0);
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
+    const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
+    if (weight == 0.f) {
+        if (lane == 0) p.loss[row] = 0.f;
+        if (GRAD) put_zeros<1, T>(g, n);
+        return;
     }
+    const ShortRow<NV, T> held(x, n);
+    if (lane < kWords) named[lane] = 0;
+    if (lane == 0) s.twice = 0;
+    __syncthreads();
+    load_entries<1, T, TT, true>(p, row, x, nullptr, 0, n, en, named, s);
+    __syncthreads();
+    sum_entries<1, REST>(p, row, en, s);
+    float m = -INFINITY;
+    bool out[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const unsigned int i = lane + 64u * j;
+        out[j] = REST && (named[i >> 5] >> (i & 31u) & 1u);
+        m = fmaxf(m, out[j] ? -INFINITY : held.v[j]);
+    }
+    m = wave_reduce(m, MaxOp{});
+    const float m0 = m > -INFINITY ? m : 0.f;
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) sum += out[j] ? 0.0 : (double)weight_of(held.v[j], m0, p.c2);
+    sum = wave_reduce(sum, SumOp{});
+    if (lane == 0) s.row[0] = MaxSum{m, sum};
+    __syncthreads();
+    finish_row<REST>(p, row, weight, s.part, 1, s.row, 1, &s.out);
+    if (!GRAD) return;
+    __syncthreads();
+    const RowScalars o = s.out;
+    const float factor = o.state == 1u ? 0.f : o.factor;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const unsigned int i = lane + 64u * j;
+        if (i < n) store_gradient(g + i, factor * weight_of(held.v[j], o.m, p.c2));
+    }
+    __syncthreads();   // (an action with an entry is written again)
+    if (o.state == 0) put_entries<1, T, REST>(p, g, en, 0, n, o, s.twice != 0);
 }
 
 template <int W, typename T, typename TT, bool REST, bool GRAD, typename Row>
@@ -468,6 +477,9 @@ __device__ __forceinline__ void distill_row(const DistillArgs& p, unsigned long 
 
 // One workgroup of W wavefronts per row, held in registers (NV > 0) or read again for each of three passes.  LDS
 // behind the arguments: the marks, (n + 31) / 32 + 1 words, and the entries.
+// Longer than 32,768 / 65,536 actions in 32 / 16 bits a row is read twice (400 x 131072 bf16: 61 us; held by 16 wavefronts of 16
+// loads 63).  The loss alone needs one pass with a running maximum and nothing held: 1000 x 50021 bf16 28 to 33 us, 3.1 to
+// 3.5 TB/s.
 template <int W, int NV, int EU, typename T, typename TT, bool REST, bool GRAD>
 __global__ __launch_bounds__(64 * W, EU) void distill_kernel(DistillArgs p) {
     extern __shared__ unsigned int lds[];
@@ -478,18 +490,16 @@ __global__ __launch_bounds__(64 * W, EU) void distill_kernel(DistillArgs p) {
                      reinterpret_cast<float*>(lds + words + 2u * k)};
     const unsigned long long row = workgroup_row();
     if (row >= p.x.rows) return;
-    {
-        const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
-        Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
-        const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
-        if (weight == 0.f) {
-            if (threadIdx.x == 0) p.loss[row] = 0.f;
-            if (GRAD) put_zeros<W, T>(g, n);
-        } else if constexpr (NV > 0) {
-            distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, HeldRow<W, NV, T, false>(x, 0, n), lds, words, en, s);
-        } else {
-            distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, ReadRow<W, W == 8 ? 8 : 4, T, false>(x, 0, n), lds, words, en, s);
-        }
+    const Global<T>* x = global_in<T>(p.x.data) + row * p.x.stride;
+    Global<T>* g = global_out<T>(p.grad) + row * p.grad_stride;
+    const float weight = p.weight ? global_in<float>(p.weight)[row] : 1.f;
+    if (weight == 0.f) {
+        if (threadIdx.x == 0) p.loss[row] = 0.f;
+        if (GRAD) put_zeros<W, T>(g, n);
+    } else if constexpr (NV > 0) {
+        distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, HeldRow<W, NV, T, false>(x, 0, n), lds, words, en, s);
+    } else {
+        distill_row<W, T, TT, REST, GRAD>(p, row, weight, x, g, ReadRow<W, W == 8 ? 8 : 4, T, false>(x, 0, n), lds, words, en, s);
     }
 }
 

@@ -653,7 +653,7 @@ def top_actions(logits, k, temperature=1.0, out=None, workspace=None, stream=Non
     """The k largest logits of every row, their actions, and the row's log-sum-exp at a temperature: see
     rp_top_actions.  Returns (values [rows, k] in the logits' type, index int32[rows, k], lse float32[rows])."""
     check_rows(logits, "top_actions: logits")
-    rows, dev = logits.shape[0], logits.device
+    rows, dev, k = logits.shape[0], logits.device, int(k)
     with _on(dev, stream):
         x = _logit_rows(logits)
         need = lib().rp_top_workspace_bytes(C.byref(x), k)

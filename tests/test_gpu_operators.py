@@ -465,6 +465,27 @@ def test_settings_may_be_numbers_of_other_kinds(B):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("rows,n", [(300_001, 30), (70_003, 70), (66_001, 300)])
+def test_more_rows_than_a_launch_has_workgroups_in_a_row(B, rows, n):
+    """Rows on both sides of 2^16 (and of 4 * 2^16, where a workgroup takes four): every row is done, and done as it would
+    be on its own."""
+    torch.manual_seed(n)
+    x = torch.randn((rows, n), device="cuda")
+    u = torch.rand(rows, device="cuda")
+    some = torch.tensor([0, 1, 65_535, 65_536, 65_537, rows // 2, rows - 2, rows - 1], device="cuda")
+    index, logp = B.choose_actions(x, u, top_p=0.9)
+    value, top, lse = B.top_actions(x, 5)
+    y = torch.randn((rows, n), device="cuda")
+    loss, grad = B.distill_grad(y, value, top, teacher_lse=lse)
+    pick = lambda t: t[some].contiguous()
+    for got, want in ((index, B.choose_actions(pick(x), pick(u), top_p=0.9)[0]), (top, B.top_actions(pick(x), 5)[1]),
+                      (grad, B.distill_grad(pick(y), pick(value), pick(top), teacher_lse=pick(lse))[1])):
+        assert torch.equal(got[some], want)
+    assert ((index >= 0) & (index < n)).all() and torch.equal(top[:, 0].long(), x.argmax(1))
+    # (rows of a gradient sum to zero: n products of 32 bits, each off by some 2^-21 of itself)
+    assert (grad.sum(1).abs() <= 2.0 ** -20 * grad.abs().sum(1) + 2.0 ** -21).all() and (loss > 0).all()
+
+
 def test_a_table_beyond_4_gib(B):
     """Offsets of the last rows pass 32 bits, in elements and in bytes."""
     n = 262_144

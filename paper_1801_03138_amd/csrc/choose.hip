@@ -1282,6 +1282,8 @@ Pieces pieces_of(unsigned long long rows, unsigned int n) {
     const unsigned int fill = (unsigned int)((512u + rows - 1u) / rows), most = n / 8192u;
     if (count < fill) count = fill < most ? fill : most > count ? most : count;
     if (count > 64u) count = 64u;
+    // (a row that stays whole is not rounded up: no whole piece of such a length would fit into it)
+    if (count == 1u) return Pieces{1u, n};
     const unsigned int length = (n / count + 63u) / 64u * 64u;
     // (the last piece takes what is left, so it must fit too)
     count = n / length;

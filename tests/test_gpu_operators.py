@@ -687,3 +687,15 @@ def test_paths_refuse_what_they_cannot_do(B):
     with pytest.raises(B.ReplayError):
         slow.act(s[:0], u[:0])
     assert np.array_equal(slow.params(), before) and slow.opt_state()[2:] == (0, 0)
+
+
+# ------------------------------------------------------------------------- lengths where a row is just not cut
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(1, 8193), (2, 10_001), (128, 12_289), (129, 10_001), (3, 16_383), (3, 16_385), (2, 32_767)])
+def test_rows_next_to_the_lengths_where_they_are_cut(B, rows, n, dtype):
+    rng = np.random.default_rng(n + rows)
+    g, x = table(rng, rows, n, dtype, pad=1, sigma=2.0, masked=0.1)
+    u = draw_u(rng, rows)
+    for how in ({"top_p": 0.9, "min_p": 0.001}, {"top_k": 40, "temperature": 0.7}, {"temperature": 0.0}):
+        check_choice(x, u, how, *B.choose_actions(g, torch.from_numpy(u).cuda(), **how))
+    check_top(x, 33, 0.7, *B.top_actions(g, 33, temperature=0.7))

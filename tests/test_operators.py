@@ -153,3 +153,26 @@ def test_the_trainers_paths_check_their_arguments():
     how = B.Choice(1.0, 1.0, 0.0, 0, None, None, None, None)
     assert lib.train_act(None, 4, P, C.byref(how), P, P, None, None, P, 1 << 20, None) == EINVAL
     assert lib.train_distill_batch(None, P, C.byref(teacher()), None) == EINVAL
+
+
+def piece_lengths():
+    """Row lengths around everything that decides how a row is cut, and all of those of one or two pieces."""
+    around = {b + d for b in range(8192, 262_145, 8192) for d in (-65, -64, -63, -1, 0, 1, 63, 64, 65)}
+    return sorted({n for n in around if n <= 262_144} | set(range(1, 130)) | set(range(8000, 17_000)))
+
+
+@pytest.mark.parametrize("dtype", [B.RP_F32, B.RP_BF16])
+@pytest.mark.parametrize("rows_", [1, 4, 32, 100, 128, 129, 1000, 2 ** 24])
+def test_every_row_length_has_a_workspace_size(rows_, dtype):
+    """Of at most 8,192 pieces with 2,048 words and a head each, and none where a workgroup holds the row and there are
+    rows for all compute units."""
+    lib, held = B.lib(), 32_768 if dtype == B.RP_BF16 else 16_384
+    for n in piece_lengths():
+        x = rows(rows=rows_, n=n, stride=n, dtype=dtype)
+        need = lib.rp_choose_workspace_bytes(C.byref(x))
+        assert need == lib.rp_top_workspace_bytes(C.byref(x), 1), n
+        assert need <= 8192 * (2048 * 8 + 32), n
+        if n <= 8192 or (n <= held and rows_ > 128):
+            assert need == 0, n
+        if n > held:
+            assert need >= min(rows_, 100) * 2 * (2048 * 8 + 32), n

@@ -520,7 +520,8 @@ Pieces pieces_of(unsigned long long rows, unsigned int n) {
     // does (about 5 us): up to 128 rows of more than 32,768 actions, 32 rows of more than 16,384.  One workgroup a
     // row -> pieces, us: 11 x 131071 fp32 44 -> 17, 128 x 50000 fp32 30 -> 27 (its loss alone 27 -> 18), 128 x 100000 bf16
     // 34 -> 30; beyond the limits 64 x 20000 fp32 13 -> 16, 128 x 32768 bf16 16 -> 18, 256 x 100000 bf16 37 -> 45.
-    if (rows > (n > 32768u ? 128u : 32u) || n <= 16384u) return Pieces{1u, n};
+    // (no rows, no pieces)
+    if (rows == 0 || rows > (n > 32768u ? 128u : 32u) || n <= 16384u) return Pieces{1u, n};
     const unsigned int most = (unsigned int)((1024u + rows - 1u) / rows);
     unsigned int count = n / 2048u;
     count = count > most ? most : count;

@@ -699,3 +699,12 @@ def test_rows_next_to_the_lengths_where_they_are_cut(B, rows, n, dtype):
     for how in ({"top_p": 0.9, "min_p": 0.001}, {"top_k": 40, "temperature": 0.7}, {"temperature": 0.0}):
         check_choice(x, u, how, *B.choose_actions(g, torch.from_numpy(u).cuda(), **how))
     check_top(x, 33, 0.7, *B.top_actions(g, 33, temperature=0.7))
+
+
+@pytest.mark.parametrize("n", [20_000, 262_144])
+def test_nothing_is_done_for_no_long_rows(B, n):
+    x = torch.empty((0, n), device="cuda")
+    assert len(B.choose_actions(x, torch.empty(0, device="cuda"))[0]) == 0
+    value, index, lse = B.top_actions(x, 4)
+    assert len(B.distill_loss(x, value, index, teacher_lse=lse)) == 0
+    assert B.distill_grad(x, value, index)[1].shape == (0, n)

@@ -176,3 +176,25 @@ def test_every_row_length_has_a_workspace_size(rows_, dtype):
             assert need == 0, n
         if n > held:
             assert need >= min(rows_, 100) * 2 * (2048 * 8 + 32), n
+
+
+@pytest.mark.parametrize("dtype", [B.RP_F32, B.RP_BF16])
+def test_no_rows_of_any_length_are_no_work(dtype):
+    lib = B.lib()
+    for n in piece_lengths():
+        x = rows(rows=0, data=None, n=n, stride=n, dtype=dtype)
+        assert lib.rp_choose_workspace_bytes(C.byref(x)) == 0 and lib.rp_top_workspace_bytes(C.byref(x), 1) == 0
+        assert lib.rp_distill_workspace_bytes(C.byref(x), 4) == 0
+        assert choose(x) == 0 and top(x, k=1) == 0 and loss(x, teacher()) == 0 and grad(x, teacher(), stride=n) == 0
+
+
+@pytest.mark.parametrize("dtype", [B.RP_F32, B.RP_BF16])
+@pytest.mark.parametrize("rows_", [1, 4, 32, 33, 128, 129, 2 ** 24])
+def test_every_row_length_has_a_workspace_size_for_distillation(rows_, dtype):
+    """Of at most 64 pieces a row, 24 bytes each, and the entries' logits, each rounded up to 256 bytes."""
+    for n in piece_lengths():
+        x = rows(rows=rows_, n=n, stride=n, dtype=dtype)
+        need = B.lib().rp_distill_workspace_bytes(C.byref(x), 7)
+        cut = n > 16_384 and rows_ <= (128 if n > 32_768 else 32)
+        assert (need > 0) == cut, n
+        assert need <= rows_ * 64 * 24 + 256 + rows_ * 7 * 4 + 256, n

@@ -59,9 +59,11 @@ struct EntryPart {
     unsigned int any;     // some entry is there with a logit above -infinity
 };
 
-// What every element's gradient needs, worked out once per row.
+// What every element's gradient needs, worked out once per row.  An element without an entry has factor exp((x - base) / ts).
+// The teacher's rest pulls at such elements with a strength that does not fall with their mass, so `base` is their own maximum
+// (REST): from the row's, exp and factor leave the range of 32 bits, to opposite sides, 87 temperatures below.
 struct RowScalars {
-    float m, factor;
+    float m, base, factor;
     double shift, q_scale, inside, scale, inv_total;
     unsigned int state;   // 0: as computed; 1: nothing to learn, all 0; 2: all NaN
 };
@@ -256,8 +258,8 @@ __device__ __forceinline__ double quarter_sum(double v) {
 }
 
 // From the parts of the row and of its entries to the loss and what the gradient needs.  Called by one wavefront.  There
-// are up to 16 parts of either kind: its quarters bring the sums over the row, over the entries' student weights and over
-// the teacher's to one maximum, with one exp for all, and one log serves for the logarithms too.
+// are up to 16 parts of either kind: its quarters bring the sums over the row, over the entries' student weights, over
+// the teacher's, and (REST) over the row to its own maximum, with one exp for all, and one log serves for the logarithms too.
 template <bool REST>
 __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long long row, float weight, const EntryPart* part,
                                            unsigned int parts, const MaxSum* rows, unsigned int pieces, RowScalars* out,
@@ -275,11 +277,15 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     const double m0 = m > -INFINITY ? (double)m : 0.0;
     const double tm = wave_reduce(own_t, MaxOp{});
     const double shift = REST ? (double)global_in<float>(p.teacher_lse)[row] : any ? tm : 0.0;
+    const double x0 = xm > -INFINITY ? (double)xm : 0.0;
     double from = quarter == 0 ? (own_x > -INFINITY ? ((double)own_x - m0) * p.inv_ts : 0.0)
+                  : REST && quarter == 3 ? (own_x > -INFINITY ? ((double)own_x - x0) * p.inv_ts : 0.0)
                   : quarter == 1 ? (own_z > -INFINITY ? ((double)own_z - m0) * p.inv_ts : 0.0)
                                  : (!REST && own_any ? (own_t - shift) * p.inv_tt : 0.0);
     const double factor = exp(from);
-    double first = quarter == 0 ? (row_here ? x.s : 0.0) : quarter == 1 ? (part_here ? r.z : 0.0) : (part_here ? r.a : 0.0);
+    double first = quarter == 0 || (REST && quarter == 3) ? (row_here ? x.s : 0.0)
+                   : quarter == 1                         ? (part_here ? r.z : 0.0)
+                                                          : (part_here ? r.a : 0.0);
     double b = part_here ? r.b : 0.0, c = part_here ? r.c : 0.0;
     // (q' (t - tm) from a wavefront's own maximum to the row's)
     if (!REST && quarter >= 2u) b = first == 0.0 ? 0.0 : (b + first * from) * factor;
@@ -290,24 +296,28 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     b = __shfl(quarter_sum(b), 32, 64);
     c = __shfl(quarter_sum(c), 32, 64);
     const double outer = __shfl(first, 0, 64), inner = __shfl(first, 16, 64), a = __shfl(first, 32, 64);
+    const double own = __shfl(first, 48, 64);   // (REST) outer, from its own maximum: 1e-20 or more, or 0 if nothing is in it
     const double total = REST ? outer + inner : outer, p_in = inner / total, p_rest = outer / total;
     // (in 64 bits log(1 - v) is as good as log1p(-v) for what is multiplied by 1 - v and added to the rest)
     const double logs = log(lane == 0   ? total
                             : lane == 1 ? (REST ? 1.0 - a : a)
                                         : (p_in < 0.5 ? 1.0 - p_in : p_rest));
     const double log_total = __shfl(logs, 0, 64), log_a = __shfl(logs, 1, 64), log_rest = __shfl(logs, 2, 64);
-    double loss, q_scale = 1.0, inside = 1.0, outside = 1.0;
+    const double scale = (double)weight * p.scale * p.inv_ts;
+    double loss, q_scale = 1.0, inside = 1.0, share = scale / total;
     if (!REST) {
         q_scale = 1.0 / a;
         loss = (b - c) * q_scale - log_a + log_total;
     } else {
         loss = b - c + a * log_total;
-        inside = outside = a;
+        inside = a;
+        double outside = a * p_rest;
         if (a < 1.0 && p_rest > 0.0) {
             loss += (1.0 - a) * (log_a - log_rest);
             inside = 1.0;
-            outside = (a - p_in) / p_rest;
+            outside = p_in < 0.5 ? a - p_in : p_rest - (1.0 - a);   // (the same number, from its smaller parts)
         }
+        share = own > 0.0 ? scale * outside / own : 0.0;
     }
     // (NaN and +infinity anywhere have made one of the sums NaN)
     const bool bad = !(total < INFINITY) || a != a;
@@ -315,9 +325,8 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     if (bad) loss = NAN;
     if (lane == 0) {
         if (put_loss) p.loss[row] = empty ? 0.f : (float)(loss * (double)weight);
-        const double scale = (double)weight * p.scale * p.inv_ts;
-        *out = RowScalars{m > -INFINITY ? m : 0.f, bad ? NAN : (float)(scale * outside / total), shift, q_scale, inside, scale,
-                          1.0 / total, empty ? 1u : bad ? 2u : 0u};
+        *out = RowScalars{m > -INFINITY ? m : 0.f, xm > -INFINITY ? xm : 0.f, bad ? NAN : (float)share, shift, q_scale,
+                          inside, scale, 1.0 / total, empty ? 1u : bad ? 2u : 0u};
     }
 }
 
@@ -332,7 +341,7 @@ __device__ __forceinline__ unsigned int bf16_pair_of(float lo, float hi) {
 // by the thread that stores it alone.
 template <typename T, typename Row>
 __device__ __forceinline__ void put_gradient(const Row& row, Global<T>* g, const RowScalars& o, float c2) {
-    const float m = o.m, factor = o.state == 1u ? 0.f : o.factor;
+    const float m = o.base, factor = o.state == 1u ? 0.f : o.factor;
     row.each_load([&](u32x4 raw, unsigned int i, unsigned int gone) {
         if constexpr (!Row::kHeld) {
             if (gone) {
@@ -447,7 +456,7 @@ __global__ __launch_bounds__(64) void distill_wave_kernel(DistillArgs p) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const unsigned int i = lane + 64u * j;
-        if (i < n) store_gradient(g + i, factor * weight_of(held.v[j], o.m, p.c2));
+        if (i < n) store_gradient(g + i, factor * weight_of(held.v[j], o.base, p.c2));
     }
     __syncthreads();   // (an action with an entry is written again)
     if (o.state == 0) put_entries<1, T, REST>(p, g, en, 0, n, o, s.twice != 0);

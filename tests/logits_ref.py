@@ -91,3 +91,42 @@ def distill(x, t, index, weight=1.0, teacher_lse=None, ts=1.0, tt=1.0):
     slack = p * reach * (unit + 2.0 ** -22 * np.abs(depth)) + 2.0 ** -24 * taken
     scale = abs(weight) / ts
     return loss * weight, g * (weight / ts), loss_slack * abs(weight) + 2.0 ** -23 * abs(loss * weight), slack * scale
+
+
+def distill_rest(x, t, index, teacher_lse, ts, tt, weight=1.0):
+    """distill with a teacher's log-sum-exp, from logarithms alone, for students whose mass outside the entries is
+    as small as it may be: (loss, gradient, slack of the loss, slack of the gradient) of one row.
+
+    The kernel's weight of an action without an entry is made from a maximum that is at most 46 + log n student temperatures
+    above the largest of them (a sum of 1e-20 or more is kept).  It is off by three roundings of its distance to that maximum,
+    under 2^-22 of it, and by under 2^-22 of itself; their sum by the mean of that, of at most log n more, and with it p_rest, the
+    total and every logarithm of them.  Weights below 2^-126 are 0: 2^-126 / 1e-20 of the sum at most."""
+    x, t, n = np.asarray(x, np.float64), np.asarray(t, np.float64), len(x)
+    there = (index >= 0) & (index < n)
+    t, j = t[there] / tt, np.asarray(index)[there]
+    named = np.zeros(n, bool)
+    named[j] = True
+    z = x / ts
+    lse, log_rest = log_sum_exp(z), log_sum_exp(z[~named])
+    log_q = t - teacher_lse
+    q = np.exp(log_q)
+    a, live = q.sum(), q > 0
+    q_rest, p_rest = 1 - a, np.exp(log_rest - lse)
+    p = np.exp(z - lse)
+    out = named | (z == -np.inf)
+    depth = np.where(out, 0.0, max(log_rest, -1e300) - np.where(out, 0.0, z))
+    share = np.where(out, 0.0, np.exp(-np.where(out, 0.0, depth)))
+    loss = (q[live] * (log_q[live] - (z[j][live] - lse))).sum()
+    reached = q_rest > 0 and log_rest > -np.inf
+    if reached:
+        loss += q_rest * (np.log(q_rest) - (log_rest - lse))
+    inside, pull = (1.0, p_rest - q_rest) if reached else (a, a * p_rest)
+    taken = np.zeros(n)
+    np.add.at(taken, j, q)
+    g = np.where(named, p * inside - taken, share * pull)
+    unit = 2.0 ** -22 * (2 * 46 + 3 * np.log(n) + 8)
+    slack = np.where(named, (p * inside + taken) * unit, share * ((unit + 2.0 ** -22 * depth) * (abs(pull) + p_rest) + 2.0 ** -48)
+                     + 2.0 ** -126 / 1e-20 * abs(pull))
+    loss_slack = unit * (a + abs(q_rest)) + 2.0 ** -23 * abs(loss) + 2.0 ** -46 * (q[live] * np.abs(z[j][live])).sum()
+    scale = abs(weight) / ts
+    return loss * weight, g * (weight / ts), loss_slack * abs(weight), slack * scale

@@ -708,3 +708,94 @@ def test_nothing_is_done_for_no_long_rows(B, n):
     value, index, lse = B.top_actions(x, 4)
     assert len(B.distill_loss(x, value, index, teacher_lse=lse)) == 0
     assert B.distill_grad(x, value, index)[1].shape == (0, n)
+
+
+# ----------------------------------------------------------------- a student that is sure of the teacher's actions
+def far_rows(rng, rows, n, k, dtype, ts, gap, mass):
+    """A student whose logits at the k named actions lie around `gap` temperatures above the others; a teacher with
+    about `mass` of its own on them."""
+    x = rng.normal(0, 1, (rows, n)) * min(1.0, 5 * ts)
+    index = np.stack([rng.permutation(n)[:k] for _ in range(rows)]).astype(np.int32)
+    np.put_along_axis(x, index, np.take_along_axis(x, index, 1) + gap * ts, 1)
+    g = torch.from_numpy(x.astype(np.float32)).to(DT[dtype]).cuda()
+    t = rng.normal(0, 1, (rows, k)).astype(np.float32)
+    lse = np.array([ref.log_sum_exp(r, 0.9) - math.log(mass) for r in t], np.float32)
+    return g, g.double().cpu().numpy(), t, index, lse
+
+
+def check_far(B, g, x, t, index, lse, dtype, ts, weight=None):
+    cuda = lambda v: None if v is None else torch.from_numpy(v).cuda()
+    kw = dict(weight=cuda(weight), teacher_lse=cuda(lse), student_temperature=ts, teacher_temperature=0.9)
+    only = B.distill_loss(g, cuda(t), cuda(index), **kw)
+    loss, grad = B.distill_grad(g, cuda(t), cuda(index), **kw)
+    own = g.clone()
+    own_loss, _ = B.distill_grad(own, cuda(t), cuda(index), out=(torch.empty_like(loss), own), **kw)
+    assert torch.isfinite(grad).all() and torch.equal(own, grad) and torch.equal(own_loss, loss)
+    loss, only, grad = loss.double().cpu().numpy(), only.double().cpu().numpy(), grad.double().cpu().numpy()
+    half, tiny = torch.finfo(DT[dtype]).eps / 2, float(torch.finfo(DT[dtype]).tiny)
+    for r in range(len(x)):
+        want, dwant, slack, dslack = ref.distill_rest(x[r], t[r], index[r], float(lse[r]), ts, 0.9,
+                                                      1.0 if weight is None else float(weight[r]))
+        assert max(abs(loss[r] - want), abs(only[r] - want)) <= slack, (r, loss[r], only[r], want, slack)
+        off = np.abs(grad[r] - dwant) - (dslack + (half + 2.0 ** -23) * np.abs(dwant) + tiny)
+        assert (off <= 0).all(), (r, int(off.argmax()), grad[r][off.argmax()], dwant[off.argmax()], float(off.max()))
+
+
+FAR_SHAPES = [(3, 30, 8), (3, 200, 20), (40, 1500, 20), (3, 5000, 1000), (33, 20_011, 64), (2, 30_000, 50), (130, 70_001, 9),
+              (3, 80_000, 300)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n,k", FAR_SHAPES)
+def test_the_rest_far_below_the_entries(B, rows, n, k, dtype):
+    """On both sides of the distances at which sums start anew, 32 bits end, and numbers below the normal ones."""
+    rng = np.random.default_rng(n)
+    for i, gap in enumerate((-20, 0, 30, 44, 60, 86, 90, 104, 300, 680) if rows * n < 2 ** 20 else (44, 60, 90, 680)):
+        ts = [1.1, 0.1, 0.01][i % 3]
+        g, x, t, index, lse = far_rows(rng, rows, n, k, dtype, ts, gap, [0.6, 0.95, 0.05, 1.2][i % 4])
+        weight = None if i % 2 else rng.choice([1.0, -0.5, 1.0 / rows], rows).astype(np.float32)
+        check_far(B, g, x, t, index, lse, dtype, ts, weight)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [30, 1500, 80_000])
+def test_a_cold_student_of_ordinary_logits(B, n, dtype):
+    """Unit normal logits at low temperatures, entries anywhere among them."""
+    rng = np.random.default_rng(n + 1)
+    g, x = table(rng, 40 if n < 10_000 else 4, n, dtype, sigma=1.0)
+    index = np.argsort(-x + rng.normal(0, 0.3, x.shape), axis=1)[:, :4].astype(np.int32)
+    t = rng.normal(0, 1, index.shape).astype(np.float32)
+    lse = np.array([ref.log_sum_exp(r, 0.9) + 0.3 for r in t], np.float32)
+    for ts in (0.1, 0.02, 0.01):
+        check_far(B, g, x, t, index, lse, dtype, ts)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_cold_student_trains(B, dtype):
+    """A layered step whose Q-values span some 600 student temperatures, the teacher's actions the best of them, backward
+    from the gradient that these very Q-values have by definition: to the tolerances of the step's products, and in mixed
+    precision of its roundings."""
+    D, H, batch, A, k = 27, 64, 64, 30, 6
+    tr = trainer(B, dtype, layered=True)
+    rng = np.random.default_rng(8)
+    s = torch.from_numpy(rng.normal(size=(batch, D)).astype(np.float32)).to(DT[dtype]).cuda()
+    t = rng.normal(0, 1, (batch, k)).astype(np.float32)
+    lse = np.array([ref.log_sum_exp(r, 0.5) + 0.5 for r in t], np.float32)
+    p0, cuda = tr.params(), lambda v: torch.from_numpy(v).cuda()
+    q = torch.empty((batch, A), device="cuda")
+    tr.act(s, torch.rand(batch, device="cuda"), q=q)
+    ts = float((q.max(1).values - q.min(1).values).max()) / 600
+    index = B.top_actions(q, k)[1].cpu().numpy()
+    tr.distill_batch(s, cuda(t), cuda(index), teacher_lse=cuda(lse), student_temperature=ts, teacher_temperature=0.5)
+    q = np.asarray(tr.last()["Q"], np.float64).reshape(-1, A)[:batch]
+    rows = [ref.distill_rest(q[i], t[i], index[i], float(lse[i]), ts, 0.5) for i in range(batch)]
+    p = torch.from_numpy(p0)
+    p = (p.to(torch.bfloat16) if dtype == "bf16" else p).double().requires_grad_()
+    z = network(p, D, H, 0, A, False, s.double().cpu())
+    (z * torch.from_numpy(np.stack([r[1] for r in rows]) / batch)).sum().backward()
+    got, want = tr.grads(), p.grad.numpy()
+    assert np.isfinite(got).all() and np.isfinite(tr.params()).all()
+    tol = 4 * 2.0 ** -24 * (D + 2 * H + batch + A) if dtype == "f32" else 12 * 2.0 ** -8
+    assert np.abs(got - want).max() <= tol * np.abs(want).max()
+    loss = np.mean([r[0] for r in rows])
+    assert abs(tr.last()["loss"] - loss) <= max(r[2] for r in rows) + 2.0 ** -22 * abs(loss)

@@ -408,7 +408,8 @@ size_t rp_distill_workspace_bytes(const rp_rows* logits, uint32_t k);
  *   else:      q_e = exp(value_e / temperature - lse), and what is missing from 1 is the teacher's mass
  *              outside its entries, set against the student's p_rest there as one more event;
  *   loss = sum_e q_e (log q_e - log p[j_e])  [ + q_rest (log q_rest - log p_rest) ],
- * times the row's weight.  The last term is left out where q_rest <= 0 or p_rest = 0.  Entries with q_e = 0
+ * times the row's weight.  The last term is left out where q_rest <= 0 or the student allows no action outside the
+ * entries (a p_rest too small for a number counts by its logarithm).  Entries with q_e = 0
  * add nothing; two entries of one action both count.  A row without entries or without an allowed
  * action in the student's row has loss 0 and gradient 0.  NaN and +infinity among the logits of a row
  * of weight other than 0, or among its entries' values, make its loss and its gradient NaN.

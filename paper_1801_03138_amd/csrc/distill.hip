@@ -298,11 +298,13 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
     const double outer = __shfl(first, 0, 64), inner = __shfl(first, 16, 64), a = __shfl(first, 32, 64);
     const double own = __shfl(first, 48, 64);   // (REST) outer, from its own maximum: 1e-20 or more, or 0 if nothing is in it
     const double total = REST ? outer + inner : outer, p_in = inner / total, p_rest = outer / total;
-    // (in 64 bits log(1 - v) is as good as log1p(-v) for what is multiplied by 1 - v and added to the rest)
+    // (in 64 bits log(1 - v) is as good as log1p(-v) for what is multiplied by 1 - v and added to the rest; p_rest itself may be
+    // below the numbers of 64 bits)
     const double logs = log(lane == 0   ? total
                             : lane == 1 ? (REST ? 1.0 - a : a)
-                                        : (p_in < 0.5 ? 1.0 - p_in : p_rest));
-    const double log_total = __shfl(logs, 0, 64), log_a = __shfl(logs, 1, 64), log_rest = __shfl(logs, 2, 64);
+                                        : (p_in < 0.5 ? 1.0 - p_in : own));
+    const double log_total = __shfl(logs, 0, 64), log_a = __shfl(logs, 1, 64), log_own = __shfl(logs, 2, 64);
+    const double log_rest = p_in < 0.5 ? log_own : log_own + (x0 - m0) * p.inv_ts - log_total;
     const double scale = (double)weight * p.scale * p.inv_ts;
     double loss, q_scale = 1.0, inside = 1.0, share = scale / total;
     if (!REST) {
@@ -312,7 +314,7 @@ __device__ __forceinline__ void finish_row(const DistillArgs& p, unsigned long l
         loss = b - c + a * log_total;
         inside = a;
         double outside = a * p_rest;
-        if (a < 1.0 && p_rest > 0.0) {
+        if (a < 1.0 && own > 0.0) {
             loss += (1.0 - a) * (log_a - log_rest);
             inside = 1.0;
             outside = p_in < 0.5 ? a - p_in : p_rest - (1.0 - a);   // (the same number, from its smaller parts)

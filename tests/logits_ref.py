@@ -106,20 +106,23 @@ def distill_rest(x, t, index, teacher_lse, ts, tt, weight=1.0):
     t, j = t[there] / tt, np.asarray(index)[there]
     named = np.zeros(n, bool)
     named[j] = True
-    z = x / ts
-    lse, log_rest = log_sum_exp(z), log_sum_exp(z[~named])
+    # (from the maximum: a log-sum-exp of 1e30 would lose the log of a sum)
+    out = named | (x == -np.inf)
+    top, own = x.max(), x[~out].max() if not out.all() else -np.inf
+    z = (x - top) / ts
+    depth = np.zeros(n) if out.all() else np.where(out, 0.0, own - np.where(out, own, x)) / ts
+    total, rest = np.exp(z).sum(), np.exp(-depth)[~out].sum()
+    log_rest = -np.inf if out.all() else (own - top) / ts + np.log(rest) - np.log(total)
+    share = np.where(out, 0.0, np.exp(-depth) / max(rest, 1e-300))
     log_q = t - teacher_lse
     q = np.exp(log_q)
     a, live = q.sum(), q > 0
-    q_rest, p_rest = 1 - a, np.exp(log_rest - lse)
-    p = np.exp(z - lse)
-    out = named | (z == -np.inf)
-    depth = np.where(out, 0.0, max(log_rest, -1e300) - np.where(out, 0.0, z))
-    share = np.where(out, 0.0, np.exp(-np.where(out, 0.0, depth)))
-    loss = (q[live] * (log_q[live] - (z[j][live] - lse))).sum()
+    q_rest, p_rest = 1 - a, np.exp(log_rest)
+    p = np.exp(z) / total
+    loss = (q[live] * (log_q[live] - (z[j][live] - np.log(total)))).sum()
     reached = q_rest > 0 and log_rest > -np.inf
     if reached:
-        loss += q_rest * (np.log(q_rest) - (log_rest - lse))
+        loss += q_rest * (np.log(q_rest) - log_rest)
     inside, pull = (1.0, p_rest - q_rest) if reached else (a, a * p_rest)
     taken = np.zeros(n)
     np.add.at(taken, j, q)
@@ -127,6 +130,6 @@ def distill_rest(x, t, index, teacher_lse, ts, tt, weight=1.0):
     unit = 2.0 ** -22 * (2 * 46 + 3 * np.log(n) + 8)
     slack = np.where(named, (p * inside + taken) * unit, share * ((unit + 2.0 ** -22 * depth) * (abs(pull) + p_rest) + 2.0 ** -48)
                      + 2.0 ** -126 / 1e-20 * abs(pull))
-    loss_slack = unit * (a + abs(q_rest)) + 2.0 ** -23 * abs(loss) + 2.0 ** -46 * (q[live] * np.abs(z[j][live])).sum()
+    loss_slack = unit * (a + abs(q_rest)) + 2.0 ** -23 * abs(loss) + 2.0 ** -46 * (q[live] * np.abs(x[j][live] / ts)).sum()
     scale = abs(weight) / ts
     return loss * weight, g * (weight / ts), loss_slack * abs(weight), slack * scale

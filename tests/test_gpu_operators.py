@@ -799,3 +799,15 @@ def test_a_cold_student_trains(B, dtype):
     assert np.abs(got - want).max() <= tol * np.abs(want).max()
     loss = np.mean([r[0] for r in rows])
     assert abs(tr.last()["loss"] - loss) <= max(r[2] for r in rows) + 2.0 ** -22 * abs(loss)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,n,k", FAR_SHAPES)
+def test_a_rest_below_the_numbers_of_64_bits(B, rows, n, k, dtype):
+    """The student's probability of the rest is no number any more; its logarithm is, and pulls."""
+    rng = np.random.default_rng(n + 2)
+    for i, (ts, gap) in enumerate(((1.1, 740), (0.01, 800), (1e-3, 5000), (1e-3, 1e5))):
+        g, x, t, index, lse = far_rows(rng, rows, n, k, dtype, ts, gap, [0.6, 0.95, 0.05, 1.2][i])
+        check_far(B, g, x, t, index, lse, dtype, ts)
+    g, x, t, index, lse = far_rows(rng, rows, n, k, dtype, 1.0, 3, 0.7)
+    check_far(B, g, x, t, index, lse, dtype, 1e-30)

@@ -363,7 +363,7 @@ size_t rp_choose_workspace_bytes(const rp_rows* logits);
  * lower index first), w_j = exp((x_j - x_0) / temperature) and C_j = w_0 + .. + w_j, an action stays
  * in if it is among the first top_k, the sum before it is less than top_p times the sum over those
  * top_k, and w_j >= min_p; the first always stays.  The choice is the first j with C_j > u * M, M
- * the sum over those that stay, or the last of them if there is none.
+ * the sum over those that stay, or the last of them if there is none (u of 1 or more); a u below 0 or NaN counts as 0.
  * index[rows]: the action, or -1 where no action is allowed.  logp[rows] (may be NULL): the logarithm
  * of its probability w_j / M (0 for index -1 and for the best action at temperature 0).
  * Weights and sums are held in 64 bits, and sums do not depend on the order in which the GPU's

@@ -173,6 +173,15 @@ __device__ void choose_by_search(const ChooseArgs& p, unsigned long long row, Se
         return above + at_count * w;
     };
 
+    // the last action that stays, by key and place among equal ones, as each limit has it; kAll: the last one with that key
+    constexpr unsigned int kAll = 0xFFFFFFFFu;
+    unsigned int last_key = lo, last_count = kAll;
+    auto ends = [&](unsigned int key, unsigned int count) {
+        if (key > last_key || (key == last_key && count < last_count)) {
+            last_key = key;
+            last_count = count;
+        }
+    };
     unsigned long long mass;
     if (k > 0 && k < (long long)allowed) {
         const unsigned int v = search_key<W>(lo, hi, [&](unsigned int v) {
@@ -183,6 +192,7 @@ __device__ void choose_by_search(const ChooseArgs& p, unsigned long long row, Se
         unsigned int c;
         search_sum<W>(x, n, m, inv_t, [&](unsigned int key) { return key > v; }, s, turn, &mass, &c);
         mass += ((unsigned int)k - c) * fixed_weight(m, key_value(v), inv_t);
+        ends(v, (unsigned int)k - c);
     } else {
         search_sum<W>(x, n, m, inv_t, [&](unsigned int) { return true; }, s, turn, &mass, nullptr);
     }
@@ -190,17 +200,30 @@ __device__ void choose_by_search(const ChooseArgs& p, unsigned long long row, Se
     if (top_p < 1.0) {
         const double need = ceil(top_p * (double)total);
         mass = reach(need >= 1.0 ? min((unsigned long long)need, total) : 1ull);
+        ends(at_key, at_count);
     }
     if (min_p > 0.0) {
         unsigned long long a;
-        search_sum<W>(x, n, m, inv_t, [&](unsigned int key) { return exp(-logit_depth(m, key_value(key), inv_t)) >= min_p; },
-                      s, turn, &a, nullptr);
+        unsigned int least = hi;   // of this thread's
+        search_sum<W>(x, n, m, inv_t, [&](unsigned int key) {
+            const bool stays = exp(-logit_depth(m, key_value(key), inv_t)) >= min_p;
+            if (stays) least = min(least, key);
+            return stays;
+        }, s, turn, &a, nullptr);
         mass = min(mass, a);
+        // (the set that the next sums do not use)
+        ends(block_reduce<W>(least, MinOp{}, s.count[turn]), min_p <= 1.0 ? kAll : 1u);
     }
     if (mass < (unsigned long long)kOne) mass = (unsigned long long)kOne;
     const float u = p.u[row];
-    const double drawn = u > 0.f ? (double)u * (double)mass : 0.0;
-    reach(drawn < (double)mass ? min((unsigned long long)drawn + 1ull, mass) : mass);
+    if (u >= 1.f) {
+        at_key = last_key;
+        at_count = last_count;
+        if (at_count == kAll) search_sum<W>(x, n, m, inv_t, [&](unsigned int key) { return key == at_key; }, s, turn, nullptr, &at_count);
+    } else {
+        const double drawn = u > 0.f ? (double)u * (double)mass : 0.0;
+        reach(min((unsigned long long)drawn + 1ull, mass));
+    }
     const unsigned int at = search_equal<W>(x, n, at_key, at_count, s);
     if (threadIdx.x == 0) {
         p.index[row] = (int)at;
@@ -493,7 +516,7 @@ struct RowChoice {
     double inv_t, top_p, min_p;
     float u;
     unsigned int k;      // 1 .. 1024: so many; 0: all
-    bool greedy, search; // search: more than 1024
+    bool greedy, search; // search: more than 1024, or the last of all that stay, which may lie below every bin
 };
 __device__ __forceinline__ RowChoice row_choice(const ChooseArgs& p, unsigned long long row) {
     RowChoice c;
@@ -511,6 +534,7 @@ __device__ __forceinline__ RowChoice row_choice(const ChooseArgs& p, unsigned lo
         c.k = k <= (long long)kMaxTop ? (unsigned int)k : 0u;
         c.search = c.k == 0u;
     }
+    c.search |= !c.k && c.u >= 1.f;
     return c;
 }
 
@@ -770,11 +794,10 @@ __device__ __forceinline__ bool choose_from_bins(const Row& row_, const ChooseAr
         bin_m = b < (double)kBins ? (unsigned int)fmax(b, 0.0) : kBins;
     }
     const unsigned int last = min(bin_p, bin_m);
-    const bool end = !(c.u < 1.f);
     // first the bin where the actions that stay end, if there is a limit, then the one of the choice
     auto round = [&](int pass) __attribute__((always_inline)) {
-        const double target = pass == 0 ? most : end ? mass : c.u > 0.f ? (double)c.u * mass : 0.0;
-        const bool past = pass == 1 && !end;
+        const double target = pass == 0 ? most : c.u > 0.f ? (double)c.u * mass : 0.0;
+        const bool past = pass == 1;
         unsigned int bin = last;
         if (pass) bin = find_bin<W>(s, [&](double v) { return past ? v > target : v >= target; });
         const float lo = bins.lo((double)bin), hi = bins.hi((double)bin);
@@ -1000,14 +1023,14 @@ __global__ __launch_bounds__(256) void choose_wave_kernel(ChooseArgs p) {
         if (rank == 0) put_choice(p, row, (int)lane, 0.f);
         return;
     }
-    const double w = allowed && (k <= 0 || (long long)rank < k) ? exp(-logit_depth(m, v, c.inv_t)) : 0.0;
+    bool stays = allowed && (k <= 0 || (long long)rank < k);
+    const double w = stays ? exp(-logit_depth(m, v, c.inv_t)) : 0.0;
     double before = 0.0, total = 0.0;
     for (unsigned int j = 0; j < n; ++j) {
         const double other = lane_value(w, (int)j);
         total += other;
         before += before_me >> j & 1ull ? other : 0.0;
     }
-    bool stays = w > 0.0;
     if (c.top_p < 1.0) stays &= before < c.top_p * total;
     if (c.min_p > 0.0) stays &= w >= c.min_p;
     stays |= rank == 0;

@@ -811,3 +811,20 @@ def test_a_rest_below_the_numbers_of_64_bits(B, rows, n, k, dtype):
         check_far(B, g, x, t, index, lse, dtype, ts)
     g, x, t, index, lse = far_rows(rng, rows, n, k, dtype, 1.0, 3, 0.7)
     check_far(B, g, x, t, index, lse, dtype, 1e-30)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [40, 65, 5000, 12_000, 50_000])
+def test_random_numbers_outside_the_unit_interval_are_its_ends_at_every_length(B, n, dtype):
+    """No number and negative ones choose the first action, one and more the last that stays, however small its weight."""
+    rng = np.random.default_rng(n)
+    u = np.array([math.nan, -1.0, 0.0, 1.0, 7.0, INF], np.float32)
+    for i, how in enumerate(({}, {"top_p": 0.9}, {"min_p": 0.02}, {"top_p": 0.6, "min_p": 0.02}, {"top_k": 7}, {"top_k": 1500},
+                             {"top_k": 1500, "top_p": 0.9, "min_p": 0.001}, {"temperature": 0.05}, {"temperature": 1e-3, "top_p": 0.99},
+                             {"temperature": 50.0, "min_p": 0.9}, {"temperature": 0.0})):
+        g, x = table(rng, len(u), n, dtype, pad=1, sigma=[2.0, 0.4][i % 2], masked=[0.0, 0.3][i % 2])
+        index, logp = B.choose_actions(g, torch.from_numpy(u).cuda(), **how)
+        for r in range(len(u)):
+            ids, c, at = ref.choose(x[r], float(u[r]), **how)
+            assert at == (len(ids) - 1 if u[r] >= 1 else 0) and int(index[r]) == ids[at], (how, r, int(index[r]), ids[at])
+        assert torch.isfinite(logp).all()

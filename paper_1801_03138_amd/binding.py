@@ -420,7 +420,7 @@ class Trainer:
         rc, dev, rows = self.replay.cfg, self.replay.device, u.numel()
         check_device_array(s, _TORCH_STATE[rc.state_dtype], rows * rc.state_dim, dev, "act: s")
         if q is not None:
-            check_device_array(q, (torch.float32,), rows * self.cfg.num_actions, dev, "act: q")
+            check_table(q, (torch.float32,), rows, self.cfg.num_actions, dev, "act: q")
         with _on(s.device, stream):
             how, u, out = _choice("act", rows, s.device, u, temperature, top_k, top_p, min_p, out)
             nbytes = int(lib().train_act_workspace_bytes(C.byref(self.cfg), rows))
@@ -560,6 +560,15 @@ def check_rows(t, what, device_type="cuda"):
     return t
 
 
+def check_table(t, dtypes, rows, n, device, what):
+    """rows x n contiguous elements on the device; a tensor with two dimensions must have these (a transposed one has as
+    many elements and would be read across its rows)."""
+    check_device_array(t, dtypes, rows * n, device, what)
+    if t.dim() == 2 and t.shape != (rows, n):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(rows, n)}")
+    return t
+
+
 def check_setting(v, dtype, rows, device, what):
     """One value for all rows, or a device array with one per row: (value, tensor or None)."""
     if isinstance(v, torch.Tensor):
@@ -663,8 +672,8 @@ def top_actions(logits, k, temperature=1.0, out=None, workspace=None, stream=Non
                    torch.empty((rows, k), dtype=torch.int32, device=dev),
                    torch.empty(rows, dtype=torch.float32, device=dev))
         values, index, lse = out
-        check_device_array(values, (logits.dtype,), rows * k, dev, "top_actions: values")
-        check_device_array(index, (torch.int32,), rows * k, dev, "top_actions: index")
+        check_table(values, (logits.dtype,), rows, k, dev, "top_actions: values")
+        check_table(index, (torch.int32,), rows, k, dev, "top_actions: index")
         if lse is not None:
             check_device_array(lse, (torch.float32,), rows, dev, "top_actions: lse")
         _check(lib().rp_top_actions(C.byref(x), k, temperature, values.data_ptr(), index.data_ptr(), _dev(lse), ws,
@@ -677,7 +686,7 @@ def _teacher(rows, dev, teacher, index, weight, teacher_lse, student_temperature
         raise ValueError(f"{what}: index must be a rows x k tensor")
     k = index.shape[1]
     check_device_array(index, (torch.int32,), rows * k, dev, what + ": index")
-    check_device_array(teacher, tuple(_LOGIT_DTYPE), rows * k, dev, what + ": teacher")
+    check_table(teacher, tuple(_LOGIT_DTYPE), rows, k, dev, what + ": teacher")
     if teacher_lse is not None:
         check_device_array(teacher_lse, (torch.float32,), rows, dev, what + ": teacher_lse")
     if weight is not None:

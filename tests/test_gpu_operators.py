@@ -828,3 +828,20 @@ def test_random_numbers_outside_the_unit_interval_are_its_ends_at_every_length(B
             ids, c, at = ref.choose(x[r], float(u[r]), **how)
             assert at == (len(ids) - 1 if u[r] >= 1 else 0) and int(index[r]) == ids[at], (how, r, int(index[r]), ids[at])
         assert torch.isfinite(logp).all()
+
+
+def test_tables_of_another_shape_are_refused(B):
+    x = torch.randn((6, 30), device="cuda")
+    value, index, lse = B.top_actions(x, 4)
+    flip = lambda t: t.reshape(4, 6)
+    for call in (lambda: B.distill_loss(x, flip(value), index), lambda: B.distill_grad(x, flip(value), index),
+                 lambda: B.distill_loss(x, value, flip(index)), lambda: B.top_actions(x, 4, out=(flip(value), index, lse)),
+                 lambda: B.top_actions(x, 4, out=(value, flip(index), lse))):
+        with pytest.raises(ValueError):
+            call()
+    tr = trainer(B, layered=True)
+    s, u = torch.randn((6, 27), device="cuda"), torch.rand(6, device="cuda")
+    with pytest.raises(ValueError):
+        tr.act(s, u, q=torch.empty((30, 6), device="cuda"))
+    flat = B.top_actions(x, 4, out=(torch.empty(24, device="cuda"), torch.empty(24, dtype=torch.int32, device="cuda"), lse))
+    assert torch.equal(flat[0].view(6, 4), value) and torch.equal(flat[1].view(6, 4), index)

@@ -198,3 +198,15 @@ def test_every_row_length_has_a_workspace_size_for_distillation(rows_, dtype):
         cut = n > 16_384 and rows_ <= (128 if n > 32_768 else 32)
         assert (need > 0) == cut, n
         assert need <= rows_ * 64 * 24 + 256 + rows_ * 7 * 4 + 256, n
+
+
+def test_the_binding_checks_shapes():
+    """A transposed table has as many elements as the right one."""
+    cpu = torch.device("cpu")
+    index = torch.zeros(4, 3, dtype=torch.int32)
+    take = lambda t: B._teacher(4, cpu, t, index, None, None, 1.0, 1.0, "t")
+    for good in (torch.zeros(4, 3), torch.zeros(12), torch.zeros(4, 3).bfloat16()):
+        take(good)
+    for bad in (torch.zeros(3, 4), torch.zeros(2, 6), torch.zeros(4, 4)[:, :3], torch.zeros(11), torch.zeros(4, 3).half()):
+        with pytest.raises(ValueError):
+            take(bad)

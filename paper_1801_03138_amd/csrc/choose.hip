@@ -777,6 +777,27 @@ __device__ __forceinline__ void locate(const Bins& bins, unsigned int b, unsigne
     __syncthreads();
 }
 
+// A row whose whole weight is with `count` equal logits, listed in LDS: sums are whole numbers, and a limit that ends exactly
+// at one of them (top-p of 1/2 over an even number) has to be met to the unit.  The choice in s.word; false if they are not
+// equal.
+template <int W>
+__device__ __forceinline__ bool choose_equal(const RowChoice& c, unsigned int count, float m, double* mass, ChooseShared<W>& s) {
+    const unsigned int tid = threadIdx.x, key = order_key(m);
+    unsigned int others = 0;
+    for (unsigned int i = tid; i < count; i += 64 * W) others |= word_key(s.words[i]) ^ key;
+    others = block_reduce<W>(others, MaxOp{}, s.search.count[0]);
+    __syncthreads();
+    if (others) return false;
+    double kept = (double)count;
+    if (c.top_p < 1.0) kept = fmax(ceil(c.top_p * kept), 1.0);
+    if (c.min_p > 1.0) kept = 1.0;
+    const unsigned int at = min((unsigned int)(c.u > 0.f ? (double)c.u * kept : 0.0), (unsigned int)kept - 1u);
+    sort_words<W>(s, count);
+    if (tid == 0) s.word = s.words[at];
+    *mass = kept;
+    return true;
+}
+
 // From the inclusive sums over bins to the choice; false if a bin holds too many actions for LDS, or, by a rounding of the
 // sums, none.
 template <int W, typename Row>
@@ -794,6 +815,9 @@ __device__ __forceinline__ bool choose_from_bins(const Row& row_, const ChooseAr
         bin_m = b < (double)kBins ? (unsigned int)fmax(b, 0.0) : kBins;
     }
     const unsigned int last = min(bin_p, bin_m);
+    // (all of it in the first bin)
+    const bool one_bin = s.sums[kBins - 1] == s.sums[0];
+    bool done = false;
     // first the bin where the actions that stay end, if there is a limit, then the one of the choice
     auto round = [&](int pass) __attribute__((always_inline)) {
         const double target = pass == 0 ? most : c.u > 0.f ? (double)c.u * mass : 0.0;
@@ -804,6 +828,10 @@ __device__ __forceinline__ bool choose_from_bins(const Row& row_, const ChooseAr
         const unsigned int count = gather_words<W>(row_, s, [&](float x) { return x >= lo && x < hi; });
         const bool find = pass == 1 || bin_p == last;
         if (count > kList || (count == 0 && find)) return false;
+        if (one_bin && bin == 0 && choose_equal<W>(c, count, m, &mass, s)) {
+            done = true;
+            return true;
+        }
         if (pass == 0 && bin_m == last) {
             // (whole numbers: their sum does not depend on the order in which the list was filled)
             unsigned long long units = 0;
@@ -826,11 +854,11 @@ __device__ __forceinline__ bool choose_from_bins(const Row& row_, const ChooseAr
         // (once in the code: twice, the compiler no longer keeps the eight loads of a thread in registers, 42 us instead of 30
         // for 1000 x 32768; the others keep theirs and lose by the loop, 52 us instead of 45 for 4096 x 1000)
 #pragma unroll 1
-        for (int pass = last < kBins ? 0 : 1; pass < 2; ++pass)
+        for (int pass = last < kBins ? 0 : 1; pass < 2 && !done; ++pass)
             if (!round(pass)) return false;
     } else {
         if (last < kBins && !round(0)) return false;
-        if (!round(1)) return false;
+        if (!done && !round(1)) return false;
     }
     if (tid == 0)
         put_choice(p, row, (int)word_index(s.word),

@@ -723,9 +723,9 @@ def far_rows(rng, rows, n, k, dtype, ts, gap, mass):
     return g, g.double().cpu().numpy(), t, index, lse
 
 
-def check_far(B, g, x, t, index, lse, dtype, ts, weight=None):
+def check_far(B, g, x, t, index, lse, dtype, ts, weight=None, tt=0.9):
     cuda = lambda v: None if v is None else torch.from_numpy(v).cuda()
-    kw = dict(weight=cuda(weight), teacher_lse=cuda(lse), student_temperature=ts, teacher_temperature=0.9)
+    kw = dict(weight=cuda(weight), teacher_lse=cuda(lse), student_temperature=ts, teacher_temperature=tt)
     only = B.distill_loss(g, cuda(t), cuda(index), **kw)
     loss, grad = B.distill_grad(g, cuda(t), cuda(index), **kw)
     own = g.clone()
@@ -734,7 +734,7 @@ def check_far(B, g, x, t, index, lse, dtype, ts, weight=None):
     loss, only, grad = loss.double().cpu().numpy(), only.double().cpu().numpy(), grad.double().cpu().numpy()
     half, tiny = torch.finfo(DT[dtype]).eps / 2, float(torch.finfo(DT[dtype]).tiny)
     for r in range(len(x)):
-        want, dwant, slack, dslack = ref.distill_rest(x[r], t[r], index[r], float(lse[r]), ts, 0.9,
+        want, dwant, slack, dslack = ref.distill_rest(x[r], t[r], index[r], float(lse[r]), ts, tt,
                                                       1.0 if weight is None else float(weight[r]))
         assert max(abs(loss[r] - want), abs(only[r] - want)) <= slack, (r, loss[r], only[r], want, slack)
         off = np.abs(grad[r] - dwant) - (dslack + (half + 2.0 ** -23) * np.abs(dwant) + tiny)
@@ -845,3 +845,101 @@ def test_tables_of_another_shape_are_refused(B):
         tr.act(s, u, q=torch.empty((30, 6), device="cuda"))
     flat = B.top_actions(x, 4, out=(torch.empty(24, device="cuda"), torch.empty(24, dtype=torch.int32, device="cuda"), lse))
     assert torch.equal(flat[0].view(6, 4), value) and torch.equal(flat[1].view(6, 4), index)
+
+
+def test_logits_that_autograd_watches(B):
+    """They are taken by their values: what comes back takes no part in automatic differentiation."""
+    x = torch.randn((5, 300), device="cuda")
+    value, index, lse = B.top_actions(x, 4)
+    y = torch.randn((5, 300), device="cuda")
+    want = B.distill_grad(y, value, index, teacher_lse=lse)
+    y.requires_grad_()
+    loss, grad = B.distill_grad(y, value, index, teacher_lse=lse)
+    assert not loss.requires_grad and not grad.requires_grad and torch.equal(loss, want[0]) and torch.equal(grad, want[1])
+    assert not B.distill_loss(y, value, index, teacher_lse=lse).requires_grad
+    y.backward(grad)   # as a program hands it on
+    assert torch.equal(y.grad, grad)
+
+
+@pytest.mark.parametrize("n", [30, 1500, 80_000])
+def test_a_cold_teacher(B, n):
+    """A log-sum-exp of thousands, in 32 bits: the loss and the gradient are those of this very number, of which the rest
+    is a small remainder."""
+    rng = np.random.default_rng(n + 3)
+    x, xs = table(rng, 6, n, "f32", sigma=1.0, shift=20.0)
+    g, gs = table(rng, 6, n, "f32", sigma=1.0)
+    for tt in (0.1, 0.01):
+        value, index, lse = B.top_actions(x, 8, temperature=tt)
+        for r in range(6):
+            assert abs(float(lse[r]) - ref.log_sum_exp(xs[r], tt)) <= 2.0 ** -23 * float(lse[r]) + 2.0 ** -22 * (math.log(n) + 4)
+        check_far(B, g, gs, value.cpu().numpy(), index.cpu().numpy(), lse.cpu().numpy(), "f32", 1.0, tt=tt)
+
+
+@pytest.mark.parametrize("dtype,H,G,A,batch,dueling,kw", [
+    ("f32", 64, 0, 30, 64, True, {}), ("f32", 256, 0, 30, 128, True, {"target_sync": 2}), ("f32", 256, 0, 30, 128, False, {}),
+    ("f32", 128, 1024, 31, 32, False, {"target_sync": 3}), ("bf16", 128, 0, 30, 64, True, {"target_sync": 2}),
+    ("bf16", 256, 128, 40, 512, False, {}), ("f32", 64, 0, 1, 64, False, {}), ("f32", 64, 0, 4096, 16, False, {})])
+def test_a_trainer_acts_after_a_run_of_steps(B, dtype, H, G, A, batch, dueling, kw):
+    """Q-values of the weights that the trainer reports, after single steps and after a run of them in one call, on a stream
+    of its own too; the bounds are those of test_a_trainer_acts_with_its_network."""
+    tr = trainer(B, dtype, H=H, G=G, A=A, batch=batch, dueling=dueling, **kw)
+    side = torch.cuda.Stream()
+    rng = np.random.default_rng(H + A)
+    for count in (1, 7, 40):
+        if count == 1:
+            assert tr.step() == 0
+        else:
+            assert tr.steps(count) == count
+        torch.cuda.synchronize()
+        s = torch.from_numpy(rng.normal(size=(130, 27)).astype(np.float32)).to(DT[dtype]).cuda()
+        u = torch.from_numpy(draw_u(rng, 130)).cuda()
+        q = torch.empty((130, A), device="cuda")
+        torch.cuda.synchronize()
+        action, logp = tr.act(s, u, temperature=0.3, q=q, stream=side)
+        torch.cuda.synchronize()
+        p = tr.params()
+        want = network(torch.from_numpy(p).double(), 27, H, G, A, dueling, s.double().cpu()).numpy()
+        got = q.double().cpu().numpy()
+        assert np.abs(got - want).max() <= 8 * 2.0 ** -24 * (27 + H + (G or H)) * np.abs(want).max()
+        check_choice(got, u.cpu().numpy(), {"temperature": 0.3}, action, logp)
+
+
+def test_a_run_of_steps_after_steps_on_a_teachers_actions(B):
+    """Steps on a teacher's actions between runs of TD steps in one call: sampling and optimizer go on where single steps
+    would, to the same weights."""
+    value, index, lse = B.top_actions(torch.randn((64, 30), device="cuda"), 5)
+    s = torch.randn((64, 27), device="cuda")
+    ends = []
+    for one_call in (False, True):
+        tr = trainer(B, layered=True, opt=B.RP_ADAM, target_sync=3)
+        for _ in range(2):
+            if one_call:
+                assert tr.steps(5) == 5
+            else:
+                for _ in range(5):
+                    assert tr.step() == 0
+            tr.distill_batch(s, value, index, teacher_lse=lse)
+        assert tr.opt_state()[2:] == (12, 12)
+        ends.append((tr.params(), tr.target()))
+    assert np.array_equal(ends[0][0], ends[1][0]) and np.array_equal(ends[0][1], ends[1][1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_top_p_of_equal_logits_ends_where_it_should(B, dtype):
+    """A constant row (an untrained network's): whole numbers, a nucleus of exactly p n actions, with and without actions
+    that are not allowed or 60 temperatures below."""
+    last = torch.tensor([1 - 2.0 ** -24, 0.0, 0.5], device="cuda")
+    for n in (30, 64, 66, 100, 160, 1000, 2048, 2052, 10_000, 60_000):
+        for value in (0.0, -3.7, 1.25, 1e6):
+            x = torch.full((3, n), value, device="cuda").to(DT[dtype])
+            for how, kept in (({"top_p": 0.5}, (n + 1) // 2), ({"top_p": 0.25, "temperature": 0.7}, (n + 3) // 4),
+                              ({"top_p": 0.75, "min_p": 0.5}, (3 * n + 3) // 4), ({"min_p": 1.0}, n), ({"min_p": 1.5}, 1), ({}, n)):
+                index, logp = B.choose_actions(x, last, **how)
+                assert index.tolist() == [kept - 1, 0, kept // 2 if kept > 1 else 0], (n, value, how)
+                assert (logp.double() + math.log(kept)).abs().max().item() <= 2.0 ** -23 * math.log(kept) + 1e-12
+            for off in (-INF, value - 60 - abs(value) * 0.1):
+                y = x.clone()
+                y[:, ::2] = off
+                kept = (n // 2 + 1) // 2
+                index, _ = B.choose_actions(y, last, top_p=0.5)
+                assert index.tolist() == [2 * kept - 1, 1, 2 * (kept // 2) + 1 if kept > 1 else 1], (n, value, off)

@@ -437,7 +437,8 @@ class Trainer:
         check_device_array(s, _TORCH_STATE[rc.state_dtype], self.cfg.batch * rc.state_dim, dev, "distill_batch: s")
         t = _teacher(self.cfg.batch, s.device, teacher, index, weight, teacher_lse, student_temperature,
                      teacher_temperature, "distill_batch")
-        return _check(lib().train_distill_batch(self._h, _dev(s), C.byref(t), _stream_ptr(stream)))
+        with _on(s.device, stream):
+            return _check(lib().train_distill_batch(self._h, _dev(s), C.byref(t), _stream_ptr(stream)))
 
     def params(self):
         p = np.empty(self.n_params, np.float32)

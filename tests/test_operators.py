@@ -210,3 +210,31 @@ def test_the_binding_checks_shapes():
     for bad in (torch.zeros(3, 4), torch.zeros(2, 6), torch.zeros(4, 4)[:, :3], torch.zeros(11), torch.zeros(4, 3).half()):
         with pytest.raises(ValueError):
             take(bad)
+
+
+def test_a_step_on_a_teachers_actions_runs_on_its_tensors_device(monkeypatch):
+    """The step's launches, and the stream it takes where none is given, belong to the device of its tensors, whichever is
+    the current one."""
+    from types import SimpleNamespace
+    seen = []
+
+    class On:
+        def __init__(self, device, stream):
+            self.device = device
+
+        def __enter__(self):
+            seen.append(("enter", self.device))
+
+        def __exit__(self, *error):
+            seen.append(("exit", self.device))
+
+    monkeypatch.setattr(B, "_on", On)
+    monkeypatch.setattr(B, "_stream_ptr", lambda stream=None: seen.append("stream"))
+    monkeypatch.setattr(B, "lib", lambda: SimpleNamespace(train_distill_batch=lambda *a: seen.append("call") or 0))
+    cpu = torch.device("cpu")
+    tr = object.__new__(B.Trainer)
+    tr._h = None
+    tr.cfg = SimpleNamespace(batch=4)
+    tr.replay = SimpleNamespace(cfg=SimpleNamespace(state_dim=27, state_dtype=B.RP_F32), device=cpu)
+    assert tr.distill_batch(torch.zeros(4, 27), torch.zeros(4, 3), torch.zeros(4, 3, dtype=torch.int32)) == 0
+    assert seen == [("enter", cpu), "stream", "call", ("exit", cpu)]

@@ -367,7 +367,9 @@ size_t rp_choose_workspace_bytes(const rp_rows* logits);
  * index[rows]: the action, or -1 where no action is allowed.  logp[rows] (may be NULL): the logarithm
  * of its probability w_j / M (0 for index -1 and for the best action at temperature 0).
  * Weights and sums are held in 64 bits, and sums do not depend on the order in which the GPU's
- * workgroups run: the same call gives the same bits.  Logits of +infinity share all weight equally.
+ * workgroups run: the same call gives the same bits.  A weight is off by 2^-43 of the best action's at most, and where u or a
+ * limit falls that close to a border either neighbour may be taken.  Logits of +infinity share all weight equally.
+ * Long rows need a workspace of up to 134 MB (16 KB for each of up to 8,192 pieces at once).
  */
 rp_status rp_choose_actions(const rp_rows* logits, const rp_choice* how, const float* u, int32_t* index,
                             float* logp, void* workspace, size_t bytes, void* hip_stream);
@@ -380,7 +382,8 @@ size_t rp_top_workspace_bytes(const rp_rows* logits, uint32_t k);
  * values[rows * k] in the logits' type and index[rows * k]; past the last allowed action -infinity and
  * -1.  lse[rows] (may be NULL): log sum_j exp(x_j / temperature) over the whole row, with
  * a temperature of 1e-30 .. 1e30 (-infinity for a row without an allowed action).  What a teacher
- * writes down for rp_distill_loss.
+ * writes down for rp_distill_loss.  It is a number of 32 bits: of size L it is off by 2^-24 L, and so is every probability made
+ * from it.  A teacher whose logits are far from 0 in units of its temperature shifts them to a maximum near 0 first.
  */
 rp_status rp_top_actions(const rp_rows* logits, uint32_t k, double temperature, void* values, int32_t* index,
                          float* lse, void* workspace, size_t bytes, void* hip_stream);

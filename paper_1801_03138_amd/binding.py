@@ -699,7 +699,8 @@ def _teacher(rows, dev, teacher, index, weight, teacher_lse, student_temperature
 def distill_loss(logits, teacher, index, weight=None, teacher_lse=None, student_temperature=1.0,
                  teacher_temperature=1.0, out=None, workspace=None, stream=None):
     """Loss of every row of the student's logits against a teacher's top logits [rows, k] and their actions, as
-    top_actions returns them: see rp_distill_loss.  Returns float32[rows]."""
+    top_actions returns them: see rp_distill_loss.  Returns float32[rows], which takes no part in autograd:
+    distill_grad gives the gradient."""
     check_rows(logits, "distill_loss: logits")
     rows, dev = logits.shape[0], logits.device
     x = _logit_rows(logits)
@@ -716,7 +717,7 @@ def distill_grad(logits, teacher, index, weight=None, teacher_lse=None, student_
                  teacher_temperature=1.0, out=None, workspace=None, stream=None):
     """distill_loss and its gradient with respect to the logits: see rp_distill_grad.  Returns (loss float32[rows],
     gradient [rows, n] in the logits' type); `out` = (loss, gradient), the gradient at any row stride, also
-    the logits themselves."""
+    the logits themselves.  Neither takes part in autograd: logits.backward(gradient) goes on from here."""
     check_rows(logits, "distill_grad: logits")
     rows, dev = logits.shape[0], logits.device
     x = _logit_rows(logits)

@@ -11,8 +11,11 @@
 // Top-k (up to 1024) and the best action: the k-th largest of the maxima of 1024 to 4096 slices of the row is a lower bound of
 // the k-th largest logit and close to it; what is not below it is sorted in LDS.  All actions: a histogram of the
 // weights, 2048 bins to 40 temperatures below the maximum; only bins where a sum ends are listed.  What these cannot take (more than
-// 1024 kept by top-k, more than 2048 actions in a bin or above the bound, +infinity) is found by binary search over the
-// values, a pass over the row for each step.
+// 1024 kept by top-k, more than 2048 actions in a bin where a sum ends or above the bound, +infinity, a random number of 1 or
+// more without top-k) is found by binary search over the values, a pass over the row for each step.  Flat rows come to that: a bin
+// is 1/51 to 1/26 of a temperature wide and holds more than 2048 of 131,072 normal logits whose deviation is under 0.5 to 1
+// temperatures.  1 x 131072 bf16 at a deviation of 0.5, top-p: 4.2 ms (torch 0.5), 256 rows 4.9 (3.7); top 2000 of one
+// row 1.8 ms (0.5), of 256 3.4 (3.7).
 #include "logits.hpp"
 
 namespace rp {
@@ -676,8 +679,9 @@ __device__ unsigned int find_bin(ChooseShared<W>& s, Reached reached) {
 }
 
 // Of the `count` actions of bin b in LDS, the first in order with which the inclusive sum over the row reaches `target` (passes
-// it, if `past`), or the last of them if rounding has it otherwise: its word and that sum, in s.word and s.part[0].  A bin
-// holds some hundred actions of a long row, so a histogram of its parts comes before anything is sorted.
+// it, if `past`), or the last of them if rounding has it otherwise: its word and that sum, in s.word and
+// s.part[0].  A bin of a long row holds some hundred actions, up to all that the list takes, so a histogram of its parts comes
+// before anything is sorted.
 template <int W>
 __device__ __forceinline__ void locate(const Bins& bins, unsigned int b, unsigned int count, double target, bool past, float m, double inv_t,
                        ChooseShared<W>& s) {
@@ -1028,7 +1032,7 @@ __device__ __forceinline__ unsigned long long lanes_before(unsigned int key, uns
     return before;
 }
 
-// (5.9 us for one row of 30, 6.9 for 128 with settings of their own: two trips to memory, and the chains of 30 sums, exp and log)
+// (5.5 us for one row of 30, 7.4 for 128 with settings of their own: two trips to memory, and the chains of 30 sums, exp and log)
 template <typename T>
 __global__ __launch_bounds__(256) void choose_wave_kernel(ChooseArgs p) {
     const unsigned int lane = threadIdx.x & 63u, n = p.x.n;
@@ -1099,7 +1103,7 @@ __global__ __launch_bounds__(256) void top_wave_kernel(TopArgs p) {
 // Long rows, and few ones: a launch brings each piece of a row to its candidates or to its histogram of weights, in the
 // workspace; a second one, a workgroup a row, joins them.  The histograms' bins lie on multiples of one width, so a piece needs
 // no other's maximum.  us of the two launches: 1 x 131072 bf16 top-k 9 + 8; 37 x 50021 fp32 top-p 8 + 25, 256 x 131072 bf16 with
-// settings of their own 30 + 36: where there is no top-k, the join reads its row again for each of the one or two bins it lists,
+// settings of their own 30 + 37: where there is no top-k, the join reads its row again for each of the one or two bins it lists,
 // on one compute unit.
 struct Pieces {
     unsigned int count, length;   // of a row; the last piece takes what is left

@@ -943,3 +943,20 @@ def test_top_p_of_equal_logits_ends_where_it_should(B, dtype):
                 kept = (n // 2 + 1) // 2
                 index, _ = B.choose_actions(y, last, top_p=0.5)
                 assert index.tolist() == [2 * kept - 1, 1, 2 * (kept // 2) + 1 if kept > 1 else 1], (n, value, off)
+
+
+def test_settings_of_rows_that_go_in_several_launches(B):
+    """More rows than the workspace has pieces for at once: each with its own settings, on both sides of the cut, as on its own."""
+    rows, n = 2800, 40_001
+    torch.manual_seed(11)
+    x, u = torch.randn((rows, n), device="cuda").mul_(2.0), torch.rand(rows, device="cuda")
+    pick = lambda v, dtype=torch.float32: torch.tensor(v, dtype=dtype, device="cuda")[torch.randint(0, len(v), (rows,), device="cuda")]
+    how = {"temperature": pick([0.0, 0.7, 1.0, 1.5]), "top_k": pick([0, 0, 3, 40, 900], torch.int32),
+           "top_p": pick([0.5, 0.9, 1.0]), "min_p": pick([0.0, 0.01, 0.1])}
+    index, logp = B.choose_actions(x, u, **how)
+    value, top, lse = B.top_actions(x, 7)
+    some = torch.cat([torch.arange(0, 5), torch.arange(2700, 2760), torch.arange(rows - 5, rows)]).cuda()
+    part = {k: v[some].contiguous() for k, v in how.items()}
+    few = x[some].contiguous()
+    check_choice(few.double().cpu().numpy(), u[some].cpu().numpy(), {k: v.cpu().numpy() for k, v in part.items()}, index[some], logp[some])
+    check_top(few.double().cpu().numpy(), 7, 1.0, value[some], top[some], lse[some])
